@@ -88,7 +88,8 @@ typedef enum {
                               the exposure. */
 } kdn_status_t;
 
-typedef enum { KDN_F32 = 0, KDN_BF16 = 1 } kdn_dtype_t;
+/* KDN_F8E4M3 is an output type of kdn_add_rmsnorm_fwd only. */
+typedef enum { KDN_F32 = 0, KDN_BF16 = 1, KDN_F8E4M3 = 2 } kdn_dtype_t;
 
 typedef struct {
   int B, T, H;           /* batch, tokens, heads */
@@ -334,6 +335,110 @@ kdn_status_t kdn_get_device_status(void *workspace, void *stream);
    kdn_get_device_status(workspace, stream) then returns KDN_ERR_TIMEOUT.
    Returns KDN_ERR_INVALID_ARG for a null or misaligned workspace. */
 kdn_status_t kdn_selftest_wait_timeout(void *workspace, void *stream);
+
+/* ==========================================================================
+ * Operators of the hybrid layer: the paper's hybrid backbone alternates the
+ * mixers above with sliding-window attention, each behind a pre-norm on the
+ * residual stream.  Same conventions (ownership, streams, errors, alignment).
+ *
+ * Sliding-window attention with sinks.  Query i of a sequence of len tokens
+ * (i < len) sees key j when j <= i and (j > i - window or j < sinks): the last
+ * `window` tokens up to itself, and the first `sinks` tokens for good.
+ *   s_ij = scale q_i.k_j;  lse_i = log sum_j exp s_ij;  o_i = sum_j exp(s_ij - lse_i) v_j
+ * over the keys i sees.  H query heads share Hk key/value heads: query head h
+ * reads kv head h / (H / Hk).
+ *   Layouts  q, o, dO, dq [B, T, H, d];  k, v, dk, dv [B, T, Hk, d]
+ *            lse [B, H, T] float32;  lens [B] int32, NULL -> every len = T
+ *            (values are clamped to [0, T])
+ *            cache kc, vc [B, Hk, sinks + window, d];  pos [B] int32
+ *   Padding  Rows at and past len see nothing and are seen by nothing: their o
+ *            and gradients are 0, their lse is -inf, and what q, k, v and dO
+ *            hold there (NaN included) is never used.
+ *   Dtypes   q, k, v, dO, o, the caches and the gradients have desc->dtype.  Scores,
+ *            softmax statistics and all sums are float32; with bfloat16 and
+ *            d = 64 or 128 the weights (and in the backward dS) are rounded to
+ *            bfloat16 as operands of the second products.
+ *   Sizes    d in {32, 64, 128}; H a multiple of Hk; T >= 0, at most 2^21; B, H <=
+ *            65535; B*H*T <= 2^31 - 1; window >= 1, sinks >= 0, window + sinks <= 2^30.
+ *   Order    Every sum has a fixed order: the same call gives the same bits.
+ */
+typedef struct {
+  int B, T, H, Hk, d; /* batch, tokens, query heads, kv heads, head dimension */
+  int window;         /* keys a query sees, itself included */
+  int sinks;          /* first tokens that every later query sees too */
+  int dtype;          /* kdn_dtype_t of q, k, v, o, dO, gradients and caches */
+  float scale;        /* > 0; NaN -> 1/sqrt(d) */
+} kdn_swa_desc_t;
+
+/* Workspace bytes of kdn_swa_fwd / kdn_swa_bwd (256-byte aligned, contents
+   need no initialisation; its first word is the device status that
+   kdn_get_device_status reads).  0 for a descriptor that is invalid or not served. */
+size_t kdn_swa_fwd_workspace_bytes(const kdn_swa_desc_t *desc);
+size_t kdn_swa_bwd_workspace_bytes(const kdn_swa_desc_t *desc);
+
+/* Forward.  lse NULL -> not written (kdn_swa_bwd needs it). */
+kdn_status_t kdn_swa_fwd(const kdn_swa_desc_t *desc, const void *q, const void *k,
+                         const void *v, const int *lens, void *o, float *lse,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of <dO, o> with respect to q, k and v from the forward's o and lse
+   (same descriptor, inputs and lens).  dk and dv are sums over the query heads
+   that share a kv head. */
+kdn_status_t kdn_swa_bwd(const kdn_swa_desc_t *desc, const void *q, const void *k,
+                         const void *v, const int *lens, const void *o, const float *lse,
+                         const void *dO, void *dq, void *dk, void *dv, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* The bounded cache of decode: like the mixers' memory its size does not grow
+   with the context.  Token t lives in slot t if t < sinks, else in slot
+   sinks + (t - sinks) mod window.  kdn_swa_cache_fill copies into it the tokens
+   of a prompt (k, v [B, T, Hk, d], lens) that a later token can still see; slots
+   that no token of the prompt belongs to are left untouched. */
+kdn_status_t kdn_swa_cache_fill(const kdn_swa_desc_t *desc, const void *k, const void *v,
+                                const int *lens, void *kc, void *vc, void *stream);
+
+/* One decode token of every sequence: q [B, H, d], k, v [B, Hk, d] are the token at
+   position pos[b] (the number of tokens before it).  Its k and v are written into
+   the cache and o [B, H, d] is its attention over the tokens it sees, itself
+   included.  pos[b] < 0: sequence b is idle, its o is 0 and its cache untouched.
+   pos is read on the device and not changed.  Slots that hold no token yet are
+   never used, whatever they hold.  desc->T is ignored; needs no workspace. */
+kdn_status_t kdn_swa_decode_step(const kdn_swa_desc_t *desc, const void *q, const void *k,
+                                 const void *v, void *kc, void *vc, const int *pos,
+                                 void *o, void *stream);
+
+/* Residual addition and RMS norm of `rows` rows of D columns:
+     h = x + res;  rstd = (mean_c h^2 + eps)^-1/2;  y = h rstd w
+   in float32, each output rounded once (y from the unrounded h).
+     out_dtype = dtype: y has the activations' type.
+     out_dtype = KDN_F8E4M3: y holds e4m3 bytes q with y ~ q * scale,
+       scale = max |y| / 448 over the row (block 0) or over each 128 columns
+       (block 128; the last block may be shorter), 1 where that maximum is 0 or
+       not finite.  scales [rows] or [rows, ceil(D / 128)] float32.
+   Sizes: D a multiple of 8, at most 16384; rows at most 2^31 - 1. */
+typedef struct {
+  long long rows;
+  int D;
+  int dtype;     /* kdn_dtype_t of x, res, h, w, dy, dh, dx: KDN_F32 or KDN_BF16 */
+  int out_dtype; /* kdn_dtype_t of y: dtype or KDN_F8E4M3 */
+  int block;     /* columns a scale: 0 (the row) or 128; KDN_F8E4M3 only */
+  float eps;     /* >= 0 */
+} kdn_norm_desc_t;
+
+/* res NULL -> h = x.  h, rstd [rows] NULL -> not written.  h may be x or res. */
+kdn_status_t kdn_add_rmsnorm_fwd(const kdn_norm_desc_t *desc, const void *x, const void *res,
+                                 const void *w, void *y, void *h, float *rstd,
+                                 float *scales, void *stream);
+
+/* Gradients: h and rstd are the forward's, dy the gradient of y, dh that of h from
+   the residual stream (NULL -> 0).  dx is the gradient of x and of res alike; dw
+   [D] float32.  dx may be dy or dh.  desc->out_dtype must be dtype (the gradient with
+   respect to the unquantised y). */
+size_t kdn_add_rmsnorm_bwd_workspace_bytes(const kdn_norm_desc_t *desc);
+kdn_status_t kdn_add_rmsnorm_bwd(const kdn_norm_desc_t *desc, const void *h, const void *w,
+                                 const float *rstd, const void *dy, const void *dh, void *dx,
+                                 float *dw, void *workspace, size_t workspace_bytes,
+                                 void *stream);
 
 #ifdef __cplusplus
 }

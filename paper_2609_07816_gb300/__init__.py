@@ -13,6 +13,9 @@ whose library is missing raises.
 Layouts follow the C ABI: q, k [B,T,H,dk]; v [B,T,H,dv]; r [B,T,H];
 diag g, omega [B,T,H,dk]; iso omega [B,T,H], g [B,T,H,dk] or [B,T,H];
 S0 [B,H,dk,dv] float32; p0 diag [B,H,dk], iso [B,H] float32.
+
+The hybrid layer's operators (sliding-window attention with sinks, the residual RMS
+norm) are at the end of the module, with their layouts.
 """
 from __future__ import annotations
 
@@ -28,7 +31,7 @@ LIB_PATH = os.path.join(_HERE, "libkdn.so")
 
 KDN_OK, KDN_ERR_INVALID_ARG, KDN_ERR_UNSUPPORTED, KDN_ERR_WORKSPACE, KDN_ERR_CUDA, \
     KDN_ERR_TIMEOUT, KDN_ERR_RANGE = range(7)
-KDN_F32, KDN_BF16 = 0, 1
+KDN_F32, KDN_BF16, KDN_F8E4M3 = 0, 1, 2
 KDN_GATES_POST, KDN_GATES_LOGITS = 0, 1
 R_MIN_DEFAULT = 0.01  # the layer's observation-noise floor
 
@@ -41,6 +44,17 @@ class kdn_desc_t(ctypes.Structure):
                 ("dtype", ctypes.c_int), ("mu", ctypes.c_float), ("scale", ctypes.c_float),
                 ("decay_per_channel", ctypes.c_int), ("out_dtype", ctypes.c_int),
                 ("gates", ctypes.c_int), ("r_min", ctypes.c_float)]
+
+
+class kdn_swa_desc_t(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int),
+                ("Hk", ctypes.c_int), ("d", ctypes.c_int), ("window", ctypes.c_int),
+                ("sinks", ctypes.c_int), ("dtype", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class kdn_norm_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("D", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("block", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 class KdnError(RuntimeError):
@@ -80,6 +94,16 @@ _SIG = {
     "kdn_get_device_status": ([_P, _P], ctypes.c_int),
     "kdn_noalloc_device_status": ([_P], ctypes.c_int),
     "kdn_selftest_wait_timeout": ([_P, _P], ctypes.c_int),
+    "kdn_swa_fwd_workspace_bytes": ([ctypes.POINTER(kdn_swa_desc_t)], ctypes.c_size_t),
+    "kdn_swa_bwd_workspace_bytes": ([ctypes.POINTER(kdn_swa_desc_t)], ctypes.c_size_t),
+    "kdn_swa_fwd": ([ctypes.POINTER(kdn_swa_desc_t)] + [_P] * 7 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "kdn_swa_bwd": ([ctypes.POINTER(kdn_swa_desc_t)] + [_P] * 11 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "kdn_swa_cache_fill": ([ctypes.POINTER(kdn_swa_desc_t)] + [_P] * 6, ctypes.c_int),
+    "kdn_swa_decode_step": ([ctypes.POINTER(kdn_swa_desc_t)] + [_P] * 8, ctypes.c_int),
+    "kdn_add_rmsnorm_fwd": ([ctypes.POINTER(kdn_norm_desc_t)] + [_P] * 8, ctypes.c_int),
+    "kdn_add_rmsnorm_bwd_workspace_bytes": ([ctypes.POINTER(kdn_norm_desc_t)], ctypes.c_size_t),
+    "kdn_add_rmsnorm_bwd": ([ctypes.POINTER(kdn_norm_desc_t)] + [_P] * 8 + [ctypes.c_size_t, _P],
+                            ctypes.c_int),
 }
 EXPORTED = tuple(_SIG)
 
@@ -568,3 +592,195 @@ def kdn_get_device_status(workspace, stream=None) -> int:
 def kdn_noalloc_device_status(stream=None) -> int:
     """Reads and clears the status word of the last kdn_diag_fwd_noalloc call."""
     return int(lib().kdn_noalloc_device_status(_stream(stream)))
+
+
+# ------------------------------------------------------------ the hybrid layer's operators
+#
+# Sliding-window attention with sinks: q, o, dO [B,T,H,d]; k, v [B,T,Hk,d], H a multiple of
+# Hk; lse [B,H,T] float32; lens [B] int32 (None: every sequence has T tokens); the decode
+# cache kc, vc [B,Hk,sinks+window,d], pos [B] int32.  Query i sees keys j <= i with
+# j > i - window or j < sinks.  Residual RMS norm: x, res, h [..., D], w [D].
+
+
+def make_swa_desc(B, T, H, Hk, d, dtype, *, window, sinks=0, scale=None) -> kdn_swa_desc_t:
+    return kdn_swa_desc_t(B, T, H, Hk, d, int(window), int(sinks), _code(dtype),
+                          math.nan if scale is None else float(scale))
+
+
+def _check_swa(q, k, v, tokens=True):
+    """q, k, v of one dtype: [B,T,H,d] and twice [B,T,Hk,d], without T for the decode step."""
+    _arg(q, "q")
+    if q.dtype not in _DTYPES:
+        raise TypeError(f"q: dtype {q.dtype}, expected torch.float32 or torch.bfloat16")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        _arg(t, name, q.dtype)
+        if t.dim() != (4 if tokens else 3):
+            raise ValueError(f"{name}: {t.dim()} dimensions, expected {4 if tokens else 3}")
+    if k.shape[:-2] != q.shape[:-2] or k.shape[-1] != q.shape[-1]:
+        raise ValueError(f"k: shape {tuple(k.shape)} does not go with q's {tuple(q.shape)}")
+    if v.shape != k.shape:
+        raise ValueError(f"v: shape {tuple(v.shape)}, expected {tuple(k.shape)}")
+
+
+def _check_cache(kc, vc, k, window, sinks):
+    shape = (k.shape[0], k.shape[-2], int(window) + int(sinks), k.shape[-1])
+    for t, name in ((kc, "kc"), (vc, "vc")):
+        _arg(t, name, k.dtype)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+
+
+def _swa_workspace(workspace, nbytes, device):
+    if workspace is None:
+        workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+    _arg(workspace, "workspace", torch.uint8)
+    return workspace
+
+
+def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=None, want_lse=True,
+                workspace=None, stream=None):
+    """Sliding-window attention with sinks over whole sequences.  Returns (o, lse); lse is
+    None with want_lse=False (kdn_swa_bwd needs it).  Rows at and past lens[b] give o = 0."""
+    _check_swa(q, k, v)
+    B, T, H, d = q.shape
+    _arg(lens, "lens", torch.int32, B, required=False)
+    desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
+    if o is None:
+        o = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
+    workspace = _swa_workspace(workspace, 256, q.device)
+    _arg(o, "o", q.dtype, q.numel())
+    _arg(lse, "lse", torch.float32, B * H * T, required=False)
+    st = lib().kdn_swa_fwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o),
+                           _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "kdn_swa_fwd")
+    return o, lse
+
+
+def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, grads=None,
+                workspace=None, stream=None):
+    """Gradients of kdn_swa_fwd from its o and lse.  Returns a dict dq, dk, dv (dk and dv
+    summed over the query heads that share a kv head)."""
+    _check_swa(q, k, v)
+    B, T, H, d = q.shape
+    _arg(lens, "lens", torch.int32, B, required=False)
+    _arg(o, "o", q.dtype, q.numel())
+    _arg(lse, "lse", torch.float32, B * H * T)
+    _arg(dO, "dO", q.dtype, q.numel())
+    desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
+    if grads is None:
+        grads = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
+    for n, x in (("dq", q), ("dk", k), ("dv", v)):
+        _arg(grads.get(n), n, q.dtype, x.numel())
+    if workspace is None:
+        workspace = _swa_workspace(None, lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc)), q.device)
+    _arg(workspace, "workspace", torch.uint8)
+    st = lib().kdn_swa_bwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o),
+                           _ptr(lse), _ptr(dO), _ptr(grads["dq"]), _ptr(grads["dk"]),
+                           _ptr(grads["dv"]), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "kdn_swa_bwd")
+    return grads
+
+
+def kdn_swa_cache_fill(k, v, kc, vc, *, window, sinks=0, lens=None, stream=None):
+    """Copies the tokens of a prompt (k, v [B,T,Hk,d]) that later tokens still see into the
+    decode cache; slots that no token of it belongs to keep what they hold."""
+    _check_swa(k, k, v)
+    B, T, Hk, d = k.shape
+    _arg(lens, "lens", torch.int32, B, required=False)
+    _check_cache(kc, vc, k, window, sinks)
+    desc = make_swa_desc(B, T, Hk, Hk, d, k.dtype, window=window, sinks=sinks)
+    st = lib().kdn_swa_cache_fill(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(lens), _ptr(kc),
+                                  _ptr(vc), _stream(stream))
+    _check(st, "kdn_swa_cache_fill")
+
+
+def kdn_swa_decode_step(q, k, v, kc, vc, pos, *, window, sinks=0, scale=None, o=None, stream=None):
+    """One token of every sequence (q [B,H,d], k, v [B,Hk,d] at position pos[b]): writes its k
+    and v into the cache in place and returns its attention o [B,H,d].  pos[b] < 0: idle."""
+    _check_swa(q, k, v, tokens=False)
+    B, H, d = q.shape
+    _arg(pos, "pos", torch.int32, B)
+    _check_cache(kc, vc, k, window, sinks)
+    desc = make_swa_desc(B, 1, H, k.shape[1], d, q.dtype, window=window, sinks=sinks, scale=scale)
+    if o is None:
+        o = torch.empty_like(q)
+    _arg(o, "o", q.dtype, q.numel())
+    st = lib().kdn_swa_decode_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(kc), _ptr(vc),
+                                   _ptr(pos), _ptr(o), _stream(stream))
+    _check(st, "kdn_swa_decode_step")
+    return o
+
+
+def _norm_desc(x, out_dtype, block, eps):
+    D = x.shape[-1]
+    return kdn_norm_desc_t(x.numel() // D if D else 0, D, _code(x.dtype), out_dtype, int(block), float(eps))
+
+
+def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=None, h=None,
+                        rstd=None, scales=None, want_rstd=True, stream=None):
+    """h = x + res and its RMS norm y = h rstd w over the last axis.  Returns (y, h, rstd,
+    scales): h is x itself without a residual; out_dtype=torch.float8_e4m3fn gives y in 8 bits
+    with float32 scales per row (block=0, [..., 1]) or per 128 columns (block=128), y ~ q * scale."""
+    _arg(x, "x")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x: dtype {x.dtype}, expected torch.float32 or torch.bfloat16")
+    if x.dim() < 1:
+        raise ValueError("x: a scalar, expected [..., D]")
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    f8 = out_dtype == torch.float8_e4m3fn
+    if not f8 and out_dtype != x.dtype:
+        raise TypeError(f"out_dtype: {out_dtype}, expected {x.dtype} or torch.float8_e4m3fn")
+    D, lead = x.shape[-1], tuple(x.shape[:-1])
+    _arg(w, "w", x.dtype, D)
+    _arg(res, "res", x.dtype, x.numel(), required=False)
+    desc = _norm_desc(x, KDN_F8E4M3 if f8 else _code(x.dtype), block, eps)
+    if y is None:
+        y = torch.empty(x.shape, dtype=out_dtype, device=x.device)
+    if h is None and res is not None:
+        h = torch.empty_like(x)
+    if rstd is None and want_rstd:
+        rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+    nb = -(-D // block) if block else 1
+    if f8 and scales is None:
+        scales = torch.empty(lead + (nb,), dtype=torch.float32, device=x.device)
+    _arg(y, "y", out_dtype, x.numel())
+    _arg(h, "h", x.dtype, x.numel(), required=False)
+    _arg(rstd, "rstd", torch.float32, desc.rows, required=False)
+    _arg(scales, "scales", torch.float32, desc.rows * nb, required=f8)
+    st = lib().kdn_add_rmsnorm_fwd(ctypes.byref(desc), _ptr(x), _ptr(res), _ptr(w), _ptr(y), _ptr(h),
+                                   _ptr(rstd), _ptr(scales), _stream(stream))
+    _check(st, "kdn_add_rmsnorm_fwd")
+    return y, x if h is None else h, rstd, scales
+
+
+def kdn_add_rmsnorm_bwd(h, w, rstd, dy, dh=None, *, dx=None, dw=None, workspace=None, stream=None):
+    """Gradients of kdn_add_rmsnorm_fwd from its h and rstd: dy is the gradient of y, dh that
+    of h from the residual stream.  Returns (dx, dw): dx for x and res alike, dw [D] float32."""
+    _arg(h, "h")
+    if h.dtype not in _DTYPES:
+        raise TypeError(f"h: dtype {h.dtype}, expected torch.float32 or torch.bfloat16")
+    if h.dim() < 1:
+        raise ValueError("h: a scalar, expected [..., D]")
+    D = h.shape[-1]
+    desc = _norm_desc(h, _code(h.dtype), 0, 0.0)
+    _arg(w, "w", h.dtype, D)
+    _arg(rstd, "rstd", torch.float32, desc.rows)
+    _arg(dy, "dy", h.dtype, h.numel())
+    _arg(dh, "dh", h.dtype, h.numel(), required=False)
+    if dx is None:
+        dx = torch.empty_like(h)
+    if dw is None:
+        dw = torch.empty(D, dtype=torch.float32, device=h.device)
+    _arg(dx, "dx", h.dtype, h.numel())
+    _arg(dw, "dw", torch.float32, D)
+    if workspace is None:
+        workspace = _swa_workspace(None, lib().kdn_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(desc)),
+                                   h.device)
+    _arg(workspace, "workspace", torch.uint8)
+    st = lib().kdn_add_rmsnorm_bwd(ctypes.byref(desc), _ptr(h), _ptr(w), _ptr(rstd), _ptr(dy), _ptr(dh),
+                                   _ptr(dx), _ptr(dw), _ptr(workspace), workspace.numel(),
+                                   _stream(stream))
+    _check(st, "kdn_add_rmsnorm_bwd")
+    return dx, dw

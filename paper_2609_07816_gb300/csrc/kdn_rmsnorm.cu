@@ -1,0 +1,315 @@
+// kdn_rmsnorm.cu -- the residual's addition with the RMS norm behind it, its output in
+// the activations' type or in 8 bits with scales, and its gradients.
+//
+//   h = x + res,  rstd = (mean h^2 + eps)^-1/2,  y = h rstd w
+//   8 bits: scale = max |y| / 448 over a row or over 128 columns, q = e4m3(y / scale)
+//   backward, g = w dy, xh = h rstd: dx = dh + rstd (g - xh mean(g xh)), dw = sum_rows dy xh
+//
+// A row is read once: TPR threads hold it in registers (EPT elements each, 16-byte
+// vectors, vector number i TPR + thread), so the statistics, the scales and the output
+// come from one pass over memory.  Sums are float32 and their order is fixed.
+// HBM traffic bounds both directions.
+#include <cuda_fp8.h>
+
+#include "kdn_internal.cuh"
+#include "kdn_rmsnorm.cuh"
+
+namespace kdn {
+namespace {
+
+constexpr float kF8Max = 448.f;  // largest finite e4m3 value
+
+template <typename DT> constexpr int EV = 16 / (int)sizeof(DT);  // elements of a 16-byte vector
+
+template <typename DT> __device__ __forceinline__ void unpack(uint4 u, float *x) {
+  if constexpr (sizeof(DT) == 4) {
+    x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y);
+    x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+  } else {
+    const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __bfloat1622float2(p[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+}
+template <typename DT> __device__ __forceinline__ uint4 pack(const float *x) {
+  uint4 u;
+  if constexpr (sizeof(DT) == 4) {
+    u = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  } else {
+    __nv_bfloat162 *p = reinterpret_cast<__nv_bfloat162 *>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+  }
+  return u;
+}
+
+// Sum (or maximum) over the TPR threads of a row.  `red` holds one float a warp and is
+// double-buffered by the caller, so one barrier a reduction is enough.
+template <int TPR, bool MAX> __device__ __forceinline__ float row_reduce(float x, float *red) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float y = __shfl_xor_sync(0xffffffffu, x, o);
+    x = MAX ? fmaxf(x, y) : x + y;
+  }
+  if constexpr (TPR > 32) {
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = x;
+    __syncthreads();
+    x = red[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 32; ++w) x = MAX ? fmaxf(x, red[w]) : x + red[w];
+  }
+  return x;
+}
+
+// threads of a CTA: eight rows of 32 threads, or one row
+template <int TPR> constexpr int CTA = TPR == 32 ? 256 : TPR;
+
+template <typename DT, int F8, int TPR, int EPT>
+__global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm(const NormArgs a) {
+  constexpr int V = EV<DT>, NV = EPT / V;
+  __shared__ float red[2][32];
+  const long long row = (long long)blockIdx.x * (CTA<TPR> / TPR) + threadIdx.x / TPR;
+  const int ln = threadIdx.x % TPR;
+  if (row >= a.rows) return;  // whole warps; with TPR > 32 a CTA is one row
+  const int nv = a.D / V;
+  const uint4 *x = static_cast<const uint4 *>(a.x) + row * nv, *w = static_cast<const uint4 *>(a.w);
+  const uint4 *r = a.res ? static_cast<const uint4 *>(a.res) + row * nv : nullptr;
+  float h[NV][V];
+  uint4 ux[NV], ur[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * TPR + ln;
+    ux[i] = c < nv ? x[c] : make_uint4(0, 0, 0, 0);
+    ur[i] = r && c < nv ? r[c] : make_uint4(0, 0, 0, 0);
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float t[V];
+    unpack<DT>(ux[i], h[i]);
+    unpack<DT>(ur[i], t);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      h[i][e] += t[e];
+      ss = fmaf(h[i][e], h[i][e], ss);
+    }
+  }
+  if (a.h) {
+    uint4 *o = static_cast<uint4 *>(a.h) + row * nv;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * TPR + ln < nv) o[i * TPR + ln] = pack<DT>(h[i]);
+  }
+  ss = row_reduce<TPR, false>(ss, red[0]);
+  const float rstd = 1.f / sqrtf(ss / (float)a.D + a.eps);
+  if (a.rstd && ln == 0) a.rstd[row] = rstd;
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float t[V];
+    const int c = i * TPR + ln;
+    unpack<DT>(c < nv ? w[c] : make_uint4(0, 0, 0, 0), t);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      h[i][e] *= rstd * t[e];
+      big = fmaxf(big, fabsf(h[i][e]));
+    }
+  }
+  if constexpr (!F8) {
+    uint4 *o = static_cast<uint4 *>(a.y) + row * nv;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * TPR + ln < nv) o[i * TPR + ln] = pack<DT>(h[i]);
+  } else {
+    // a block of 128 columns is 128 / V consecutive lanes of one warp
+    const int nb = a.block ? (a.D + 127) / 128 : 1;
+    if (!a.block) big = row_reduce<TPR, true>(big, red[1]);
+    unsigned char *o = static_cast<unsigned char *>(a.y) + row * a.D;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * TPR + ln;
+      if (a.block) {
+        big = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) big = fmaxf(big, fabsf(h[i][e]));
+#pragma unroll
+        for (int s = 64 / V; s > 0; s >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, s));
+      }
+      // an all-zero block has scale 1; so has one whose magnitudes are not finite (its
+      // elements are NaN: a row with an infinity or a NaN has no finite norm)
+      const bool ok = big > 0.f && big < INFINITY;
+      const float scale = ok ? big / kF8Max : 1.f;
+      if (c < nv) {
+        unsigned char q[V];
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const __nv_fp8x2_storage_t p = __nv_cvt_float2_to_fp8x2(
+              make_float2(h[i][e] / scale, h[i][e + 1] / scale), __NV_SATFINITE, __NV_E4M3);
+          q[e] = (unsigned char)(p & 0xff);
+          q[e + 1] = (unsigned char)(p >> 8);
+        }
+        if constexpr (V == 8) *reinterpret_cast<uint2 *>(o + c * V) = *reinterpret_cast<const uint2 *>(q);
+        else *reinterpret_cast<uint32_t *>(o + c * V) = *reinterpret_cast<const uint32_t *>(q);
+        if (a.block ? (c * V) % 128 == 0 : c == 0) a.scales[row * nb + (a.block ? c * V / 128 : 0)] = scale;
+      }
+    }
+  }
+}
+
+// Rows are dealt out to the CTAs in turn; dw stays in registers across a CTA's rows
+// and leaves as one float32 row of partial sums a CTA.  The next row's loads are in
+// flight while the current one is reduced.
+template <typename DT, int TPR, int EPT>
+__global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm_bwd(const NormArgs a) {
+  constexpr int V = EV<DT>, NV = EPT / V, RPC = CTA<TPR> / TPR;
+  __shared__ float red[2][32];
+  __shared__ __align__(16) float s_dw[RPC > 1 ? RPC * 32 * EPT : 1];
+  const int ln = threadIdx.x % TPR, sub = threadIdx.x / TPR, nv = a.D / V;
+  const uint4 *w = static_cast<const uint4 *>(a.w);
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  float dw[NV][V] = {};
+  uint4 uh[NV], uy[NV], ud[NV];
+  auto load = [&](long long row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * TPR + ln;
+      const bool ok = row < a.rows && c < nv;
+      uh[i] = ok ? static_cast<const uint4 *>(a.hin)[row * nv + c] : zero;
+      uy[i] = ok ? static_cast<const uint4 *>(a.dy)[row * nv + c] : zero;
+      ud[i] = ok && a.dh ? static_cast<const uint4 *>(a.dh)[row * nv + c] : zero;
+    }
+  };
+  const long long step = (long long)gridDim.x * RPC;
+  long long row = (long long)blockIdx.x * RPC + sub;
+  load(row);
+  int par = 0;
+  for (; row < a.rows; row += step, par ^= 1) {
+    const float rstd = a.rstd_in[row];
+    float xh[NV][V], g[NV][V], dh[NV][V], dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * TPR + ln;
+      float t[V];
+      unpack<DT>(uh[i], xh[i]);
+      unpack<DT>(uy[i], g[i]);
+      unpack<DT>(ud[i], dh[i]);
+      unpack<DT>(c < nv ? w[c] : zero, t);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        xh[i][e] *= rstd;
+        dw[i][e] = fmaf(g[i][e], xh[i][e], dw[i][e]);
+        g[i][e] *= t[e];
+        dot = fmaf(g[i][e], xh[i][e], dot);
+      }
+    }
+    load(row + step);
+    dot = row_reduce<TPR, false>(dot, red[par]) / (float)a.D;
+    uint4 *o = static_cast<uint4 *>(a.dx) + row * nv;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) dh[i][e] = fmaf(rstd, fmaf(-dot, xh[i][e], g[i][e]), dh[i][e]);
+      if (i * TPR + ln < nv) o[i * TPR + ln] = pack<DT>(dh[i]);
+    }
+  }
+  float *part = a.part + (size_t)blockIdx.x * a.D;
+  if constexpr (RPC == 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * TPR + ln;
+      if (c < nv)
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[c * V + e] = dw[i][e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s_dw[sub * 32 * EPT + (i * TPR + ln) * V + e] = dw[i][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.D; c += CTA<TPR>) {
+      float x = 0.f;
+#pragma unroll
+      for (int r = 0; r < RPC; ++r) x += s_dw[r * 32 * EPT + c];
+      part[c] = x;
+    }
+  }
+}
+
+// dw: the CTAs' partial rows added in order, 32 columns a CTA.
+__global__ void __launch_bounds__(1024) k_rmsnorm_dw(const float *part, int n, int D, float *dw) {
+  __shared__ float s[32][33];
+  const int cx = threadIdx.x % 32, ry = threadIdx.x / 32, c = blockIdx.x * 32 + cx;
+  float x = 0.f;
+  if (c < D)
+    for (int r = ry; r < n; r += 32) x += part[(size_t)r * D + c];
+  s[ry][cx] = x;
+  __syncthreads();
+  if (ry == 0 && c < D) {
+    float y = 0.f;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) y += s[r][cx];
+    dw[c] = y;
+  }
+}
+
+kdn_status_t launched() { return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA; }
+
+// Threads a row and elements a thread: a warp a row up to 1024 columns (no barrier),
+// else 128 threads (up to 4096) or 512.
+template <int TPR, int EPT> struct Shape { static constexpr int tpr = TPR, ept = EPT; };
+template <typename F> kdn_status_t by_shape(int D, F f) {
+  if (D <= 256) return f(Shape<32, 8>{});
+  if (D <= 512) return f(Shape<32, 16>{});
+  if (D <= 1024) return f(Shape<32, 32>{});
+  if (D <= 2048) return f(Shape<128, 16>{});
+  if (D <= 4096) return f(Shape<128, 32>{});
+  if (D <= 8192) return f(Shape<512, 16>{});
+  return f(Shape<512, 32>{});
+}
+
+template <typename DT, int F8> kdn_status_t fwd_t(const NormArgs &a, cudaStream_t s) {
+  return by_shape(a.D, [&](auto sh) {
+    constexpr int TPR = decltype(sh)::tpr, EPT = decltype(sh)::ept, RPC = CTA<TPR> / TPR;
+    k_add_rmsnorm<DT, F8, TPR, EPT><<<(unsigned)((a.rows + RPC - 1) / RPC), CTA<TPR>, 0, s>>>(a);
+    return launched();
+  });
+}
+
+template <typename DT> kdn_status_t bwd_t(const NormArgs &a, cudaStream_t s) {
+  const int n = rmsnorm_bwd_blocks(a.rows, a.D);
+  if (n) {
+    const kdn_status_t st = by_shape(a.D, [&](auto sh) {
+      constexpr int TPR = decltype(sh)::tpr, EPT = decltype(sh)::ept;
+      k_add_rmsnorm_bwd<DT, TPR, EPT><<<n, CTA<TPR>, 0, s>>>(a);
+      return launched();
+    });
+    if (st != KDN_OK) return st;
+  }
+  k_rmsnorm_dw<<<(a.D + 31) / 32, 1024, 0, s>>>(a.part, n, a.D, a.dw);
+  return launched();
+}
+
+}  // namespace
+
+// CTAs of the backward: enough to fill the GPU, each with its own row of partial sums.
+int rmsnorm_bwd_blocks(long long rows, int D) {
+  const long long rpc = D <= 1024 ? 8 : 1, full = 152LL * (D <= 1024 ? 4 : D <= 4096 ? 5 : 2);
+  const long long n = (rows + rpc - 1) / rpc;
+  return (int)(n < full ? n : full);
+}
+
+kdn_status_t launch_add_rmsnorm(const NormArgs &a, cudaStream_t s) {
+  if (a.dtype == KDN_BF16) return a.f8 ? fwd_t<__nv_bfloat16, 1>(a, s) : fwd_t<__nv_bfloat16, 0>(a, s);
+  return a.f8 ? fwd_t<float, 1>(a, s) : fwd_t<float, 0>(a, s);
+}
+
+kdn_status_t launch_add_rmsnorm_bwd(const NormArgs &a, cudaStream_t s) {
+  return a.dtype == KDN_BF16 ? bwd_t<__nv_bfloat16>(a, s) : bwd_t<float>(a, s);
+}
+
+}  // namespace kdn

@@ -1,0 +1,566 @@
+// kdn_swa_general.cu -- sliding-window attention with sinks on the CUDA cores:
+// float32 activations (any head dimension) and bfloat16 with d = 32, float32
+// arithmetic throughout; and the parts that every path shares (the backward's
+// row sums, the join of split key tiles, the copy of a prompt into the cache).
+//
+//   s_ij = c q_i.k_j,  o_i = sum_j exp(s_ij - lse_i) v_j   over the keys that i sees
+//   dS = P (dO V^T - delta), dQ = c dS K, dK = c dS^T Q, dV = P^T dO
+//
+// Tiles are 64 queries x 64 keys, 256 threads; thread (ty, tx) owns rows ty + 16 i
+// and columns tx + 16 j of a 64 x 64 product (i, j < 4), so that with rows of d + 4
+// floats both operands' 16-byte reads are free of bank conflicts, and two such
+// reads feed 16 multiply-adds.  The multiply-add rate bounds these kernels.
+#include "kdn_swa.cuh"
+
+namespace kdn {
+
+SwaSplits swa_splits(const SwaArgs &a, int BM, int BN) {
+  SwaSplits p{};
+  auto cdiv = [](long long x, long long y) { return (int)((x + y - 1) / y); };
+  p.tiles = cdiv(a.T, BN);
+  const int qtiles = cdiv(a.T, BM);
+  p.sink_tiles = cdiv(a.ns < a.T ? a.ns : a.T, BN);
+  const long long reach = (long long)a.W + BN - 2;  // last query of a window tile, from its first key
+  const int nq = (int)(reach / BM + 1 < qtiles ? reach / BM + 1 : qtiles);
+  const int iters = a.G * nq, iters_sink = a.G * qtiles;
+  // Split a tile's iterations when there are fewer tiles than SMs.  A split pays for
+  // writing and re-reading 8 BN d bytes of partial sums, about three iterations' time.
+  const long long whole = (long long)a.B * a.Hk * p.tiles;
+  int want = whole >= 152 ? 1 : cdiv(152, whole > 0 ? whole : 1);
+  if (want > iters / 4) want = iters / 4 > 0 ? iters / 4 : 1;
+  p.per = cdiv(iters, want);
+  p.splits = cdiv(iters, p.per);
+  // The sinks' tiles are seen by all later queries: cut to the length of the others,
+  // unless that is within twice theirs.
+  p.per_sink = (p.splits == 1 && iters_sink <= 2 * iters) ? iters_sink : p.per;
+  p.splits_sink = cdiv(iters_sink, p.per_sink);
+  p.blocks = p.sink_tiles * p.splits_sink + (p.tiles - p.sink_tiles) * p.splits;
+  p.part_blocks = p.splits > 1 ? p.blocks : p.splits_sink > 1 ? p.sink_tiles * p.splits_sink : 0;
+  return p;
+}
+
+namespace {
+
+constexpr int BT = kSwaGenTile, NT = 256, LP = BT + 4;  // LP: row stride of a 64 x 64 tile
+
+template <int D> constexpr int LD = D + 4;
+
+// acc[i][j] += sum_d A[ty + 16 i][d] B[tx + 16 j][d]
+template <int D>
+__device__ __forceinline__ void mm_nt(float (&acc)[4][4], const float *A, const float *B, int ty, int tx) {
+#pragma unroll 4
+  for (int d = 0; d < D; d += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = *reinterpret_cast<const float4 *>(A + (ty + 16 * i) * LD<D> + d);
+      y[i] = *reinterpret_cast<const float4 *>(B + (tx + 16 * i) * LD<D> + d);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
+        acc[i][j] = fmaf(x[i].y, y[j].y, acc[i][j]);
+        acc[i][j] = fmaf(x[i].z, y[j].z, acc[i][j]);
+        acc[i][j] = fmaf(x[i].w, y[j].w, acc[i][j]);
+      }
+  }
+}
+
+// Column of entry c (of d / 16) that thread tx owns in a [64][d] product: groups of
+// four (two for d = 32) consecutive columns.
+template <int D> constexpr int VW = D >= 64 ? 4 : 2;
+template <int D> __device__ __forceinline__ int col_of(int tx, int c) {
+  return (c / VW<D>) * 16 * VW<D> + tx * VW<D> + c % VW<D>;
+}
+
+// acc[i][c] += sum_k P[ty + 16 i][k] X[k][col(c)]
+template <int D>
+__device__ __forceinline__ void mm_nn(float (&acc)[4][D / 16], const float *P, const float *X, int ty, int tx) {
+  constexpr int NC = D / 16;
+#pragma unroll 4
+  for (int k = 0; k < BT; k += 4) {
+    float p[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 t = *reinterpret_cast<const float4 *>(P + (ty + 16 * i) * LP + k);
+      p[i][0] = t.x; p[i][1] = t.y; p[i][2] = t.z; p[i][3] = t.w;
+    }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      float x[NC];
+#pragma unroll
+      for (int c = 0; c < NC; c += VW<D>) {
+        const float *src = X + (k + kk) * LD<D> + col_of<D>(tx, c);
+        if constexpr (VW<D> == 4) {
+          const float4 t = *reinterpret_cast<const float4 *>(src);
+          x[c] = t.x; x[c + 1] = t.y; x[c + 2] = t.z; x[c + 3] = t.w;
+        } else {
+          const float2 t = *reinterpret_cast<const float2 *>(src);
+          x[c] = t.x; x[c + 1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[i][c] = fmaf(p[i][kk], x[c], acc[i][c]);
+    }
+  }
+}
+
+// Rows [r0, r0 + 64) of head h of a [B, T, heads, D] tensor into a float32 tile;
+// rows at and past `len` as zeros (whatever memory holds there).
+template <typename DT, int D>
+__device__ __forceinline__ void load_tile(float *dst, const void *src, int b, int h, int heads, int T, int r0,
+                                          int len) {
+  constexpr int V4 = D / 4;
+  for (int e = threadIdx.x; e < BT * V4; e += NT) {
+    const int r = e / V4, c = (e % V4) * 4, t = r0 + r;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (t < len) {
+      const size_t at = (((size_t)b * T + t) * heads + h) * D + c;
+      if constexpr (sizeof(DT) == 4) {
+        x = *reinterpret_cast<const float4 *>(static_cast<const float *>(src) + at);
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(src) + at);
+        const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x));
+        const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y));
+        x = make_float4(lo.x, lo.y, hi.x, hi.y);
+      }
+    }
+    *reinterpret_cast<float4 *>(dst + r * LD<D> + c) = x;
+  }
+}
+
+// sum / max over the 16 threads of a row (tx = 0..15 of a half-warp)
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+__device__ __forceinline__ float row_max(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+
+template <int D> constexpr int FWD_SMEM = (2 * BT * LD<D> + (BT * LD<D> > BT * LP ? BT * LD<D> : BT * LP)) * 4;
+
+template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_fwd(const SwaArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  float *sq = sm, *sv = sq + BT * LD<D>, *sk = sv + BT * LD<D>, *sp = sk;  // P takes K's place
+  constexpr int NC = D / 16;
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const int b = blockIdx.z, h = blockIdx.y, hk = h / a.G, i0 = blockIdx.x * BT;
+  const int len = swa_len(a, b), i1 = min(i0 + BT, len);
+  float o[4][NC] = {}, m[4], l[4] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
+  if (i0 < len) {
+    load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
+    const SwaKeyTiles kt(i0, i1, a.W, a.ns, BT);
+    const float c2 = a.scale * kLog2e;
+    for (int n = 0; n < kt.count; ++n) {
+      const int j0 = kt.at(n) * BT;
+      __syncthreads();
+      load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+      load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+      __syncthreads();
+      float s[4][4] = {};
+      mm_nt<D>(s, sq, sk, ty, tx);
+      __syncthreads();  // K has been read: P may take its place
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int qi = i0 + ty + 16 * i;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kj = j0 + tx + 16 * j;
+          s[i][j] = (qi < len && swa_sees(qi, kj, a.W, a.ns)) ? s[i][j] * c2 : -INFINITY;
+          mx = fmaxf(mx, s[i][j]);
+        }
+        const float mn = fmaxf(m[i], row_max(mx));
+        const float ref = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing yet
+        const float f = exp2f(m[i] - ref);
+        m[i] = mn;
+        l[i] *= f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[i][c] *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = exp2f(s[i][j] - ref);
+          l[i] += p;
+          sp[(ty + 16 * i) * LP + tx + 16 * j] = p;
+        }
+      }
+      __syncthreads();
+      mm_nn<D>(o, sp, sv, ty, tx);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int qi = i0 + ty + 16 * i;
+    const float ls = row_sum(l[i]);
+    if (qi >= a.T) continue;
+    const bool live = qi < len;
+    const float inv = live ? 1.f / ls : 0.f;
+    const size_t at = (((size_t)b * a.T + qi) * a.H + h) * D;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) st<DT>(a.o, at + col_of<D>(tx, c), live ? o[i][c] * inv : 0.f);
+    if (a.lse && tx == 0)
+      a.lse[((size_t)b * a.H + h) * a.T + qi] = live ? (m[i] + log2f(ls)) * kLn2 : -INFINITY;
+  }
+}
+
+template <int D> constexpr int BWD_SMEM = (4 * BT * LD<D> + BT * LP + 2 * BT) * 4;
+
+// dQ of a query tile: one pass over the keys that it sees.
+template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq(const SwaArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  float *sq = sm, *sg = sq + BT * LD<D>, *sk = sg + BT * LD<D>, *sv = sk + BT * LD<D>, *sd = sv + BT * LD<D>;
+  constexpr int NC = D / 16;
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const int b = blockIdx.z, h = blockIdx.y, hk = h / a.G, i0 = blockIdx.x * BT;
+  const int len = swa_len(a, b), i1 = min(i0 + BT, len);
+  float acc[4][NC] = {};
+  if (i0 < len) {
+    load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
+    load_tile<DT, D>(sg, a.dO, b, h, a.H, a.T, i0, len);
+    const size_t row0 = ((size_t)b * a.H + h) * a.T;
+    float nl[4], de[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int qi = i0 + ty + 16 * i;
+      nl[i] = qi < len ? a.nlse[row0 + qi] : INFINITY;
+      de[i] = qi < len ? a.delta[row0 + qi] : 0.f;
+    }
+    const SwaKeyTiles kt(i0, i1, a.W, a.ns, BT);
+    const float c2 = a.scale * kLog2e;
+    for (int n = 0; n < kt.count; ++n) {
+      const int j0 = kt.at(n) * BT;
+      __syncthreads();
+      load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+      load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+      __syncthreads();
+      float s[4][4] = {}, dp[4][4] = {};
+      mm_nt<D>(s, sq, sk, ty, tx);
+      mm_nt<D>(dp, sg, sv, ty, tx);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int qi = i0 + ty + 16 * i, kj = j0 + tx + 16 * j;
+          const bool see = qi < len && swa_sees(qi, kj, a.W, a.ns);
+          const float p = see ? exp2f(fmaf(s[i][j], c2, -nl[i])) : 0.f;
+          sd[(ty + 16 * i) * LP + tx + 16 * j] = see ? p * (dp[i][j] - de[i]) : 0.f;
+        }
+      __syncthreads();
+      mm_nn<D>(acc, sd, sk, ty, tx);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int qi = i0 + ty + 16 * i;
+    if (qi >= a.T) continue;
+    const size_t at = (((size_t)b * a.T + qi) * a.H + h) * D;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) st<DT>(a.dq, at + col_of<D>(tx, c), acc[i][c] * a.scale);
+  }
+}
+
+// dK and dV of a split of a key tile: one pass over (query head of the group, query
+// tile) pairs.  Thread (ty, tx) holds P^T and dS^T of keys ty + 16 i, queries tx + 16 j.
+template <typename DT, int D>
+__global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSplits sp) {
+  extern __shared__ __align__(16) float sm[];
+  float *sk = sm, *sv = sk + BT * LD<D>, *sq = sv + BT * LD<D>, *sg = sq + BT * LD<D>, *st_ = sg + BT * LD<D>;
+  float *snl = st_ + BT * LP, *sde = snl + BT;
+  constexpr int NC = D / 16;
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const int b = blockIdx.z, hk = blockIdx.y, x = blockIdx.x;
+  const int nsx = sp.sink_tiles * sp.splits_sink;
+  const int t = x < nsx ? x / sp.splits_sink : sp.sink_tiles + (x - nsx) / sp.splits;
+  const int split = x < nsx ? x % sp.splits_sink : (x - nsx) % sp.splits;
+  const int per = x < nsx ? sp.per_sink : sp.per;
+  const int len = swa_len(a, b), j0 = t * BT;
+  float dk[4][NC] = {}, dv[4][NC] = {};
+  if (j0 < len) {
+    int first, last;
+    swa_query_tiles(t, BT, BT, a.W, a.ns, len, &first, &last);
+    const int nq = last - first + 1;
+    const int it1 = min((split + 1) * per, a.G * nq);
+    const float c2 = a.scale * kLog2e;
+    load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+    load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+    for (int it = split * per; it < it1; ++it) {
+      const int h = hk * a.G + it / nq, i0 = (first + it % nq) * BT;
+      const size_t row0 = ((size_t)b * a.H + h) * a.T;
+      __syncthreads();
+      load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
+      load_tile<DT, D>(sg, a.dO, b, h, a.H, a.T, i0, len);
+      if (tid < BT) {
+        snl[tid] = i0 + tid < len ? a.nlse[row0 + i0 + tid] : INFINITY;
+        sde[tid] = i0 + tid < len ? a.delta[row0 + i0 + tid] : 0.f;
+      }
+      __syncthreads();
+      float s[4][4] = {}, dp[4][4] = {};
+      mm_nt<D>(s, sk, sq, ty, tx);
+      mm_nt<D>(dp, sv, sg, ty, tx);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kj = j0 + ty + 16 * i, qc = tx + 16 * j, qi = i0 + qc;
+          const bool see = qi < len && swa_sees(qi, kj, a.W, a.ns);
+          s[i][j] = see ? exp2f(fmaf(s[i][j], c2, -snl[qc])) : 0.f;
+          dp[i][j] = see ? s[i][j] * (dp[i][j] - sde[qc]) : 0.f;
+          st_[(ty + 16 * i) * LP + qc] = s[i][j];
+        }
+      __syncthreads();
+      mm_nn<D>(dv, st_, sg, ty, tx);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st_[(ty + 16 * i) * LP + tx + 16 * j] = dp[i][j];
+      __syncthreads();
+      mm_nn<D>(dk, st_, sq, ty, tx);
+    }
+  }
+  if (x < sp.part_blocks) {
+    float *part = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x) * (2 * BT * D);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int e = (ty + 16 * i) * D + col_of<D>(tx, c);
+        part[e] = dk[i][c];
+        part[BT * D + e] = dv[i][c];
+      }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int kj = j0 + ty + 16 * i;
+    if (kj >= a.T) continue;
+    const size_t at = (((size_t)b * a.T + kj) * a.Hk + hk) * D;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      st<DT>(a.dk, at + col_of<D>(tx, c), dk[i][c] * a.scale);
+      st<DT>(a.dv, at + col_of<D>(tx, c), dv[i][c]);
+    }
+  }
+}
+
+// delta_i = sum_d o_id dO_id, and lse in log2 units: one warp a row, rows in memory
+// order.  Rows past the length (and rows whose lse says that they see nothing) get
+// +inf, so that their weights are exp2(-inf) = 0.  Reads 2 d elements a row: bandwidth.
+template <typename DT> __global__ void __launch_bounds__(NT) k_swa_prep(const SwaArgs a) {
+  const size_t row = (size_t)blockIdx.x * (NT / 32) + threadIdx.x / 32, rows = (size_t)a.B * a.T * a.H;
+  const int lane = threadIdx.x % 32;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+  if (row >= rows) return;
+  const int h = (int)(row % a.H);
+  const size_t bt = row / a.H;
+  const int t = (int)(bt % a.T), b = (int)(bt / a.T);
+  const size_t out = ((size_t)b * a.H + h) * a.T + t;
+  if (t >= swa_len(a, b)) {
+    if (lane == 0) { a.nlse[out] = INFINITY; a.delta[out] = 0.f; }
+    return;
+  }
+  float x = 0.f;
+  for (int c = 2 * lane; c < a.d; c += 64) {
+    x = fmaf(ld<DT>(a.o, row * a.d + c), ld<DT>(a.dO, row * a.d + c), x);
+    x = fmaf(ld<DT>(a.o, row * a.d + c + 1), ld<DT>(a.dO, row * a.d + c + 1), x);
+  }
+  x = warp_sum(x);
+  if (lane == 0) {
+    const float l = a.lse[out];
+    a.nlse[out] = l == -INFINITY ? INFINITY : l * kLog2e;
+    a.delta[out] = x;
+  }
+}
+
+// dk, dv of split key tiles: their partial sums added in split order.
+template <typename DT> __global__ void __launch_bounds__(NT) k_swa_join(const SwaArgs a, const SwaSplits sp, int BN) {
+  const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
+  const bool sink = t < sp.sink_tiles;
+  const int n = sink ? sp.splits_sink : sp.splits;
+  const int x0 = sink ? t * n : sp.sink_tiles * sp.splits_sink + (t - sp.sink_tiles) * n;
+  const int len = swa_len(a, b);
+  const size_t one = (size_t)2 * BN * a.d;
+  const float *part = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x0) * one;
+  for (int e = threadIdx.x; e < BN * a.d; e += NT) {
+    const int j = t * BN + e / a.d;
+    if (j >= a.T) break;
+    float k = 0.f, v = 0.f;
+    for (int s = 0; s < n; ++s) {
+      k += part[s * one + e];
+      v += part[s * one + BN * a.d + e];
+    }
+    const size_t at = (((size_t)b * a.T + j) * a.Hk + hk) * a.d + e % a.d;
+    st<DT>(a.dk, at, j < len ? k * a.scale : 0.f);
+    st<DT>(a.dv, at, j < len ? v : 0.f);
+  }
+}
+
+// Copies the tokens of a prompt that decode still sees into the cache's slots:
+// token t < s to slot t, later ones to slot s + (t - s) mod W, the newest W of them.
+// Slots that no token of the prompt belongs to are left as they are.
+__global__ void __launch_bounds__(NT) k_swa_cache_fill(const SwaArgs a, uint4 *kc, uint4 *vc, int v16) {
+  const int b = blockIdx.z, hk = blockIdx.y, len = swa_len(a, b);
+  const size_t S = (size_t)a.W + a.ns;
+  const size_t n = (size_t)min((long long)len, (long long)S) * v16;  // filled slots come first
+  for (size_t e = (size_t)blockIdx.x * NT + threadIdx.x; e < n; e += (size_t)gridDim.x * NT) {
+    const int slot = (int)(e / v16), c = (int)(e % v16);
+    // the newest token of the slot: the last t < len with (t - s) mod W = slot - s
+    const int t = slot < a.ns ? slot : slot + (len - 1 - slot) / a.W * a.W;
+    const size_t from = (((size_t)b * a.T + t) * a.Hk + hk) * v16 + c;
+    const size_t to = (((size_t)b * a.Hk + hk) * S + slot) * v16 + c;
+    kc[to] = static_cast<const uint4 *>(a.k)[from];
+    vc[to] = static_cast<const uint4 *>(a.v)[from];
+  }
+}
+
+// One token over the cache: 8 lanes a key (d / 8 channels each), 32 keys at a time in
+// the CTA's 8 warps, a running softmax per group of lanes, joined through shared
+// memory.  One CTA owns one query head; the group's first head writes the new token
+// into its slot, and every head takes that slot's row from the inputs.
+template <typename DT, int D>
+__global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, void *vc, const int *pos) {
+  constexpr int E = D / 8, GR = NT / 8;
+  __shared__ float s_m[GR], s_l[GR], s_o[GR][D];
+  const int tid = threadIdx.x, gr = tid / 8, ln = tid % 8;
+  const int h = blockIdx.x, b = blockIdx.y, hk = h / a.G;
+  const int p = pos[b];
+  const size_t out = ((size_t)b * a.H + h) * D;
+  if (p < 0) {
+    if (tid < D) st<DT>(a.o, out + tid, 0.f);
+    return;
+  }
+  const size_t S = (size_t)a.W + a.ns;
+  const int slot = p < a.ns ? p : a.ns + (p - a.ns) % a.W;
+  const int n = (int)min((long long)p + 1, (long long)S);
+  const size_t base = ((size_t)b * a.Hk + hk) * S * D, in = ((size_t)b * a.Hk + hk) * D;
+  if (h % a.G == 0 && tid < D) {
+    static_cast<DT *>(kc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.k)[in + tid];
+    static_cast<DT *>(vc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.v)[in + tid];
+  }
+  // lane's channels: E / 4 runs of four, 32 apart
+  const float c2 = a.scale * kLog2e;
+  float q[E], o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    q[e] = ld<DT>(a.q, out + 32 * (e / 4) + 4 * ln + e % 4) * c2;
+    o[e] = 0.f;
+  }
+  for (int j0 = 0; j0 < n; j0 += GR) {  // the same trip count for every lane
+    const int j = j0 + gr;
+    const bool live = j < n;
+    const void *kp = j == slot ? a.k : kc, *vp = j == slot ? a.v : vc;
+    const size_t at = j == slot ? in : base + (size_t)(live ? j : 0) * D;
+    float s = 0.f, v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const size_t x = at + 32 * (e / 4) + 4 * ln + e % 4;
+      s = fmaf(q[e], live ? ld<DT>(kp, x) : 0.f, s);
+      v[e] = live ? ld<DT>(vp, x) : 0.f;
+    }
+#pragma unroll
+    for (int w = 4; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
+    if (!live) continue;
+    const float mn = fmaxf(m, s), f = exp2f(m - mn), pr = exp2f(s - mn);
+    m = mn;
+    l = fmaf(l, f, pr);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], f, pr * v[e]);
+  }
+  if (ln == 0) { s_m[gr] = m; s_l[gr] = l; }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_o[gr][32 * (e / 4) + 4 * ln + e % 4] = o[e];
+  __syncthreads();
+  if (tid < D) {
+    float mm = s_m[0], ls = 0.f, x = 0.f;  // group 0 always has the first key
+    for (int g = 1; g < GR; ++g) mm = fmaxf(mm, s_m[g]);
+    for (int g = 0; g < GR; ++g) {
+      const float f = exp2f(s_m[g] - mm);
+      ls = fmaf(s_l[g], f, ls);
+      x = fmaf(s_o[g][tid], f, x);
+    }
+    st<DT>(a.o, out + tid, x / ls);
+  }
+}
+
+kdn_status_t launched() { return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA; }
+
+template <typename K> bool smem_ok(K kernel, int bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+}
+
+template <typename DT, int D> kdn_status_t fwd_t(const SwaArgs &a, cudaStream_t s) {
+  if (!smem_ok(k_swa_fwd<DT, D>, FWD_SMEM<D>)) return KDN_ERR_CUDA;
+  k_swa_fwd<DT, D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, FWD_SMEM<D>, s>>>(a);
+  return launched();
+}
+
+template <typename DT, int D> kdn_status_t bwd_t(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
+  if (!smem_ok(k_swa_bwd_dq<DT, D>, BWD_SMEM<D>) || !smem_ok(k_swa_bwd_dkv<DT, D>, BWD_SMEM<D>)) return KDN_ERR_CUDA;
+  k_swa_bwd_dkv<DT, D><<<dim3(sp.blocks, a.Hk, a.B), NT, BWD_SMEM<D>, s>>>(a, sp);
+  k_swa_bwd_dq<DT, D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, BWD_SMEM<D>, s>>>(a);
+  return launched();
+}
+
+template <typename DT, int D>
+kdn_status_t dec_t(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
+  k_swa_decode<DT, D><<<dim3(a.H, a.B), NT, 0, s>>>(a, kc, vc, pos);
+  return launched();
+}
+
+}  // namespace
+
+#define KDN_SWA_BY_TYPE(fn, ...)                                                        \
+  do {                                                                                  \
+    if (a.dtype == KDN_BF16)                                                            \
+      return a.d == 128  ? fn<__nv_bfloat16, 128>(__VA_ARGS__)                          \
+             : a.d == 64 ? fn<__nv_bfloat16, 64>(__VA_ARGS__)                           \
+                         : fn<__nv_bfloat16, 32>(__VA_ARGS__);                          \
+    return a.d == 128 ? fn<float, 128>(__VA_ARGS__)                                     \
+           : a.d == 64 ? fn<float, 64>(__VA_ARGS__) : fn<float, 32>(__VA_ARGS__);       \
+  } while (0)
+
+kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s) { KDN_SWA_BY_TYPE(fwd_t, a, s); }
+
+kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
+  KDN_SWA_BY_TYPE(bwd_t, a, sp, s);
+}
+
+kdn_status_t launch_swa_decode_general(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
+  KDN_SWA_BY_TYPE(dec_t, a, kc, vc, pos, s);
+}
+
+kdn_status_t launch_swa_prep(const SwaArgs &a, cudaStream_t s) {
+  const size_t rows = (size_t)a.B * a.T * a.H;
+  const unsigned grid = (unsigned)((rows + NT / 32 - 1) / (NT / 32));
+  if (a.dtype == KDN_BF16) k_swa_prep<__nv_bfloat16><<<grid, NT, 0, s>>>(a);
+  else k_swa_prep<float><<<grid, NT, 0, s>>>(a);
+  return launched();
+}
+
+kdn_status_t launch_swa_join(const SwaArgs &a, const SwaSplits &sp, int BN, cudaStream_t s) {
+  if (!sp.part_blocks) return KDN_OK;
+  const dim3 grid(sp.splits > 1 ? sp.tiles : sp.sink_tiles, a.Hk, a.B);
+  if (a.dtype == KDN_BF16) k_swa_join<__nv_bfloat16><<<grid, NT, 0, s>>>(a, sp, BN);
+  else k_swa_join<float><<<grid, NT, 0, s>>>(a, sp, BN);
+  return launched();
+}
+
+kdn_status_t launch_swa_cache_fill(const SwaArgs &a, void *kc, void *vc, cudaStream_t s) {
+  const int v16 = a.d * (a.dtype == KDN_BF16 ? 2 : 4) / 16;
+  const long long most = ((long long)a.W + a.ns < a.T ? (long long)a.W + a.ns : a.T) * v16;
+  const unsigned gx = (unsigned)((most + 4 * NT - 1) / (4 * NT));
+  k_swa_cache_fill<<<dim3(gx, a.Hk, a.B), NT, 0, s>>>(a, static_cast<uint4 *>(kc), static_cast<uint4 *>(vc), v16);
+  return launched();
+}
+
+}  // namespace kdn
