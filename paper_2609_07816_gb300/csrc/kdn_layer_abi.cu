@@ -117,7 +117,7 @@ kdn_status_t kdn_swa_fwd(const kdn_swa_desc_t *desc, const void *q, const void *
   a.status = static_cast<unsigned *>(workspace);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cudaMemsetAsync(a.status, 0, sizeof(unsigned), s) != cudaSuccess) return KDN_ERR_CUDA;
-  return launch_swa_fwd_general(a, s);
+  return swa_tc_supported(a) ? launch_swa_fwd_tc(a, s) : launch_swa_fwd_general(a, s);
 }
 
 kdn_status_t kdn_swa_bwd(const kdn_swa_desc_t *desc, const void *q, const void *k, const void *v, const int *lens,

@@ -76,7 +76,9 @@ __host__ __device__ inline void swa_query_tiles(int t, int BN, int BM, int W, in
 
 SwaSplits swa_splits(const SwaArgs &a, int BM, int BN);
 
+// bfloat16 with d = 64 or 128 runs on the tensor cores
 bool swa_tc_supported(const SwaArgs &a);
+kdn_status_t launch_swa_fwd_tc(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
 // delta, nlse and a cleared status word: the first launch of every backward

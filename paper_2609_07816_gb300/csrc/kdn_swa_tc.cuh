@@ -1,0 +1,154 @@
+// kdn_swa_tc.cuh -- what the tensor-core kernels of the sliding-window attention share:
+// TMEM accesses of 32 columns, products with the A operand in TMEM, packed float32
+// arithmetic, and the TMA descriptor of 128 tokens of one head.
+#pragma once
+
+#include "kdn_fused_common.cuh"
+#include "kdn_swa.cuh"
+
+namespace kdn {
+namespace swa {
+
+using namespace sm103;
+using fused::chunk_off;
+using fused::sm16;
+
+constexpr uint32_t kWait = 1u << 25;  // polls of a bounded wait (seconds), as in the other fused kernels
+constexpr int TILE = 128;             // queries of an accumulator, keys of a tile
+constexpr int SLAB = TILE * 128;      // 128 rows of 64 bf16: one 128-byte-swizzled slab
+
+// 32 lanes x 32 columns; the registers are valid after tmem_ld_wait(r).
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+        "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+        "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+// Ties 32 registers to this point of the program: what a load wrote into them is not
+// used before it.
+__device__ __forceinline__ void pin32(float *v) {
+  asm volatile(""
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
+                 "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
+                 "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
+                 "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
+}
+template <int N> __device__ __forceinline__ void tmem_ld_wait(float *v) {  // N registers, a multiple of 32
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i += 32) pin32(v + i);
+}
+__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t *v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *v) {
+  tmem_st16(taddr, v);
+  tmem_st16(taddr + 16, v + 16);
+}
+
+// D(tmem) (+)= A(tmem) * B(smem desc): A holds 128 rows (lanes), two 16-bit elements of
+// the K axis a column.
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two float32 multiply-adds (additions) in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long &>(d))
+      : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)),
+        "l"(reinterpret_cast<unsigned long long &>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long &>(d))
+      : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long &>(d))
+      : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_bf2(float lo, float hi) {
+  uint32_t u;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+  return u;
+}
+
+// Barrier of the 128 (or 256) threads that share `id`.
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// A bounded wait that gives up for the whole CTA: the first role whose wait runs out
+// raises `fail` (shared memory) and records the timeout; the others see it and leave.
+struct Waiter {
+  volatile int *fail;
+  unsigned *status;
+  __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
+    for (uint32_t i = 0; i < kWait; ++i) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if (i > 256) {
+        if (*fail) return false;
+        __nanosleep(64);
+      }
+    }
+    *fail = 1;
+    atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
+    return false;
+  }
+  // the same answer for all lanes of a warp
+  __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
+    return __all_sync(0xffffffffu, (*this)(bar, parity));
+  }
+};
+
+// Rows [first, 128) of a tile of `slabs` slabs set to zero by one warp: tokens past a
+// sequence's length hold anything, and a weight of zero does not hide a NaN.
+__device__ __forceinline__ void zero_rows(unsigned char *tile, int slabs, int first, int lane) {
+  for (int s = 0; s < slabs; ++s)
+    for (int c = first * 8 + lane; c < TILE * 8; c += 32)
+      *reinterpret_cast<uint4 *>(tile + s * SLAB + c * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// TMA descriptor of a [B, T, heads, d] bf16 tensor; box: 64 channels of one head, 128 tokens.
+inline bool token_map(CUtensorMap *m, const void *p, int B, int T, int heads, int d) {
+  auto enc = fused::encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)B};
+  const cuuint64_t strides[3] = {(cuuint64_t)d * 2, (cuuint64_t)heads * d * 2, (cuuint64_t)T * heads * d * 2};
+  const cuuint32_t box[4] = {64, 1, TILE, 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(p), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace swa
+}  // namespace kdn
