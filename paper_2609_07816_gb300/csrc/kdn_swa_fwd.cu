@@ -47,8 +47,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   unsigned char *sq = sm, *sk = sm + 2 * TB, *sv = sk + NS * TB;
   uint64_t *bars = reinterpret_cast<uint64_t *>(sv + NS * TB);
   uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS;
-  uint64_t *s_full = v_empty + NS, *p_full = s_full + 2, *o_full = p_full + 2, *q_full = o_full + 2;
-  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(q_full + 1);
+  uint64_t *s_full = v_empty + NS, *p_full = s_full + 2, *o_full = p_full + 2, *q_full = o_full + 2, *v_clean = q_full + 1;
+  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(v_clean + 1);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(o_full + i, 1);
     }
     mbar_init(q_full, 1);
+    mbar_init(v_clean, 1);
     *s_fail = 0;
     fence_mbar_init();
     prefetch_tmap(&mq);
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const Waiter wait{s_fail, a.status};
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8 && N > 0) {
       if (lane == 0) {  // ------------------------------------------------ loads
         mbar_expect_tx(q_full, (half[1].last >= 0 ? 2 : 1) * TB);
@@ -114,66 +115,69 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int m = max(0, n - NS); m < n; ++m) mbar_wait(v_full + m % NS, (m / NS) & 1, kWait >> 6);
         }
       }
-    } else if (warp == 9 && N > 0) {  // ---------------------------------- products
-      const uint32_t id_s = idesc_bf16(TILE, TILE, 0, 0), id_o = idesc_bf16(TILE, D, 0, 1);
-      const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), av = smem_u32(sv);
-      int pending[2] = {-1, -1}, done[2] = {0, 0}, zeroed = -1;
-      uint32_t used = 0;  // stages whose V one of two accumulators has used
-      bool ok = wait.warp(q_full, 0);
-      // O_x += P_x V of tile number m of the list; the P is the accumulator's done[x]-th
-      auto pv = [&](int x, int m) {
-        const int st = m % NS, j0 = kt.at(m) * TILE;
-        // V is free when the last accumulator that needs it has used it
-        const bool both = half[0].needs(kt.at(m)) && half[1].needs(kt.at(m));
-        const bool last_use = !both || (used >> st & 1);
-        if (both) used ^= 1u << st;
-        if (!wait.warp(p_full + x, done[x] & 1) || !wait.warp(v_full + st, (m / NS) & 1)) return false;
-        if (j0 + TILE > len && len < a.T && zeroed != m) {
-          zero_rows(sv + st * TB, SL, len - j0, lane);
+      __syncwarp();
+      if (len < a.T && kt.at(N - 1) * TILE + TILE > len) {  // the last tile's V past the length
+        const int st = (N - 1) % NS;
+        if (wait.warp(v_full + st, ((N - 1) / NS) & 1)) {
+          zero_rows(sv + st * TB, SL, len % TILE, lane);
           fence_proxy_async();
-          zeroed = m;
-        }
-        __syncwarp();
-        tc_fence_after();
-        if (lane == 0) {
-#pragma unroll
-          for (int kk = 0; kk < TILE / 16; ++kk)
-            umma_ts(tb + 256 + x * 128, tb + x * 128 + kk * 8, sw128_desc(av + st * TB + kk * 2048, SLAB, 1024), id_o,
-                    done[x] > 0 || kk > 0);
-          if (last_use) umma_commit(v_empty + st);
-          umma_commit(o_full + x);
-        }
-        __syncwarp();
-        ++done[x];
-        return true;
-      };
-      for (int n = 0; ok && n < N; ++n) {
-        const int st = n % NS, t = kt.at(n);
-        for (int x = 0; ok && x < 2; ++x) {
-          if (!half[x].needs(t)) continue;
-          if (pending[x] >= 0) ok = pv(x, pending[x]);
-          ok = ok && wait.warp(k_full + st, (n / NS) & 1);
-          if (!ok) break;
-          tc_fence_after();
-          if (lane == 0) {
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
-              umma_bf16(tb + x * 128, sw128_desc(aq + x * TB + o, 16, 1024), sw128_desc(ak + st * TB + o, 16, 1024),
-                        id_s, kk > 0);
-            }
-            if (x == 1 || !half[1].needs(t)) umma_commit(k_empty + st);
-            umma_commit(s_full + x);
-          }
           __syncwarp();
-          pending[x] = n;
+          if (lane == 0) mbar_arrive(v_clean);
         }
       }
-      for (int x = 0; ok && x < 2; ++x)
-        if (pending[x] >= 0) ok = pv(x, pending[x]);
+    } else if (warp == 9 && N > 0) {  // ---------------------------------- products
+      if (elect_one()) {
+        const uint32_t id_s = idesc_bf16(TILE, TILE, 0, 0), id_o = idesc_bf16(TILE, D, 0, 1);
+        const uint64_t dq = desc_k(sq), dk = desc_k(sk), dv = desc_mn(sv);
+        int pending[2] = {-1, -1}, done[2] = {0, 0};
+        uint32_t used = 0;  // stages whose V one of two accumulators has used
+        bool ok = wait(q_full, 0);
+        // O_x += P_x V of tile number m of the list; the P is the accumulator's done[x]-th
+        auto pv = [&](int x, int m) {
+          const int st = m % NS, t = kt.at(m);
+          // V is free when the last accumulator that needs it has used it
+          const bool both = half[0].needs(t) && half[1].needs(t);
+          const bool last_use = !both || (used >> st & 1);
+          if (both) used ^= 1u << st;
+          if (!wait(v_full + st, (m / NS) & 1)) return false;
+          if (t * TILE + TILE > len && len < a.T && !wait(v_clean, 0)) return false;
+          if (!wait(p_full + x, done[x] & 1)) return false;
+          tc_fence_after();
+          const uint64_t d = dv + st * (TB >> 4);
+          const uint32_t acc = done[x] > 0;
+#pragma unroll
+          for (int kk = 0; kk < TILE / 16; ++kk)
+            umma_ts(tb + 256 + x * 128, tb + x * 128 + kk * 8, d + step_mn(kk), id_o, kk ? 1u : acc);
+          if (last_use) umma_commit(v_empty + st);
+          ++done[x];
+          return true;
+        };
+        for (int n = 0; ok && n < N; ++n) {
+          const int st = n % NS, t = kt.at(n);
+          if (!(ok = wait(k_full + st, (n / NS) & 1))) break;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (!half[x].needs(t)) continue;
+            if (pending[x] >= 0 && !(ok = pv(x, pending[x]))) break;
+            const uint64_t d = dk + st * (TB >> 4), e = dq + x * (TB >> 4);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              umma_bf16(tb + x * 128, e + step_k(kk), d + step_k(kk), id_s, kk > 0);
+            umma_commit(s_full + x);
+            if (x == 1 || !half[1].needs(t)) umma_commit(k_empty + st);
+            pending[x] = n;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (ok && pending[x] >= 0) {
+            ok = pv(x, pending[x]);
+            umma_commit(o_full + x);
+          }
+      }
     }
   } else {  // ------------------------------------------------------------- softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int x = warp >> 2, r = tid & 127, r0 = i0 + x * TILE, i = r0 + r;
     const uint32_t ts = tb + x * 128 + ((uint32_t)(32 * (warp & 3)) << 16), to = ts + 256;
     const float c2 = a.scale * kLog2e;
@@ -191,10 +195,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int c = 0; c < TILE; c += 32) tmem_ld32(ts + c, s + c);
       tmem_ld_wait<TILE>(s);
       if (t == hx.last || j0 + a.W <= r0 + TILE - 1) {  // some query does not see some key
-        const int hi = i - j0, lo = hi - a.W, sk_ = a.ns - j0;
 #pragma unroll
-        for (int c = 0; c < TILE; ++c)
-          if (!(c <= hi && (c > lo || c < sk_))) s[c] = -INFINITY;
+        for (int c = 0; c < TILE; c += 32) {
+          const uint32_t see = key_bits(i - j0 - c, a.W, a.ns - j0 - c);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[c + e] = (see >> e & 1u) ? s[c + e] : -INFINITY;
+        }
       }
       float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -246,7 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_arrive(p_full + x);
       ++k;
     }
-    if (ok && k > 0) ok = wait.warp(o_full + x, (k - 1) & 1);
+    if (ok && k > 0) ok = wait.warp(o_full + x, 0);
     // o through shared memory (this accumulator's queries are no longer needed there)
     unsigned char *so = sq + x * TB;
     if (ok && r0 < a.T) {

@@ -68,6 +68,24 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       : "memory");
 }
 
+// One lane of a converged warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+// A value that is the same in every lane, in a form the compiler knows to be.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// Descriptors of a [128][64 n] tile in 128-byte-swizzled slabs, as a sum of a part that is
+// formed once and the offset of a K step, so that a product issues with one addition:
+// K along the 64-element rows (its step kk of 16 elements) ...
+__device__ __forceinline__ uint64_t desc_k(const void *tile) { return sw128_desc(smem_u32(tile), 16, 1024); }
+__device__ __forceinline__ constexpr uint64_t step_k(int kk) { return ((kk >> 2) * SLAB + (kk & 3) * 32) >> 4; }
+// ... or along the 128 rows (the M or N axis along the 64-element rows).
+__device__ __forceinline__ uint64_t desc_mn(const void *tile) { return sw128_desc(smem_u32(tile), SLAB, 1024); }
+__device__ __forceinline__ constexpr uint64_t step_mn(int kk) { return (kk * 2048) >> 4; }
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -102,6 +120,14 @@ __device__ __forceinline__ uint32_t pack_bf2(float lo, float hi) {
   return u;
 }
 
+// The first n bits of a word (n of any size).
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u; }
+// Bits of 32 consecutive keys that a query sees; key 0 of them lies `hi` before it
+// (hi < 0: behind it), and `sinks` of them are sinks.
+__device__ __forceinline__ uint32_t key_bits(int hi, int W, int sinks) {
+  return low_bits(hi + 1) & (~low_bits(hi - W + 1) | low_bits(sinks));
+}
+
 // Barrier of the 128 (or 256) threads that share `id`.
 __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
@@ -109,20 +135,23 @@ __device__ __forceinline__ void named_sync(int id, int threads) {
 
 // A bounded wait that gives up for the whole CTA: the first role whose wait runs out
 // raises `fail` (shared memory) and records the timeout; the others see it and leave.
+__device__ __forceinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *fail, unsigned *status) {
+  for (uint32_t i = 0; i < kWait; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (i > 256) {
+      if (*fail) return false;
+      __nanosleep(64);
+    }
+  }
+  *fail = 1;
+  atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
+  return false;
+}
 struct Waiter {
   volatile int *fail;
   unsigned *status;
   __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
-    for (uint32_t i = 0; i < kWait; ++i) {
-      if (mbar_try_wait(bar, parity)) return true;
-      if (i > 256) {
-        if (*fail) return false;
-        __nanosleep(64);
-      }
-    }
-    *fail = 1;
-    atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
-    return false;
+    return mbar_try_wait(bar, parity) || mbar_try_wait(bar, parity) || wait_slow(bar, parity, fail, status);
   }
   // the same answer for all lanes of a warp
   __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
