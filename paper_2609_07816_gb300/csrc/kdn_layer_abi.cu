@@ -102,7 +102,8 @@ size_t kdn_swa_bwd_workspace_bytes(const kdn_swa_desc_t *desc) {
   SwaArgs a;
   if (fill_swa(desc, true, &a) != KDN_OK) return 0;
   if (!has_work(a)) return kAlign;
-  return swa_bwd_layout(&a, swa_splits(a, kSwaGenTile, kSwaGenTile), kSwaGenTile, nullptr);
+  const int BN = swa_tc_supported(a) ? kSwaTcTile : kSwaGenTile;
+  return swa_bwd_layout(&a, swa_splits(a, BN, BN), BN, nullptr);
 }
 
 kdn_status_t kdn_swa_fwd(const kdn_swa_desc_t *desc, const void *q, const void *k, const void *v, const int *lens,
@@ -128,7 +129,8 @@ kdn_status_t kdn_swa_bwd(const kdn_swa_desc_t *desc, const void *q, const void *
   if (st != KDN_OK) return st;
   if (!has_work(a)) return KDN_OK;
   if (!ptrs_ok({q, k, v, o, lse, dO, dq, dk, dv}, {lens})) return KDN_ERR_INVALID_ARG;
-  const int BN = kSwaGenTile;
+  const bool tc = swa_tc_supported(a);
+  const int BN = tc ? kSwaTcTile : kSwaGenTile;
   const SwaSplits sp = swa_splits(a, BN, BN);
   if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < swa_bwd_layout(&a, sp, BN, nullptr))
     return KDN_ERR_WORKSPACE;
@@ -137,7 +139,7 @@ kdn_status_t kdn_swa_bwd(const kdn_swa_desc_t *desc, const void *q, const void *
   a.dO = dO; a.dq = dq; a.dk = dk; a.dv = dv;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((st = launch_swa_prep(a, s)) != KDN_OK) return st;
-  if ((st = launch_swa_bwd_general(a, sp, s)) != KDN_OK) return st;
+  if ((st = tc ? launch_swa_bwd_tc(a, sp, s) : launch_swa_bwd_general(a, sp, s)) != KDN_OK) return st;
   return launch_swa_join(a, sp, BN, s);
 }
 

@@ -79,6 +79,8 @@ SwaSplits swa_splits(const SwaArgs &a, int BM, int BN);
 // bfloat16 with d = 64 or 128 runs on the tensor cores
 bool swa_tc_supported(const SwaArgs &a);
 kdn_status_t launch_swa_fwd_tc(const SwaArgs &a, cudaStream_t s);
+kdn_status_t launch_swa_bwd_tc(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
+constexpr int kSwaTcTile = 128;  // query and key tile of the tensor-core kernels
 kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
 // delta, nlse and a cleared status word: the first launch of every backward
