@@ -76,6 +76,19 @@ __host__ __device__ inline void swa_query_tiles(int t, int BN, int BM, int W, in
 
 SwaSplits swa_splits(const SwaArgs &a, int BM, int BN);
 
+// Rows of key tile t (tiles of BN queries and keys) that split number `split` adds to: a
+// split of a sink tile whose queries all lie past the tile's window only has the sinks'.
+__device__ __forceinline__ int swa_split_rows(int t, int split, int per, int BN, int W, int ns, int G, int len) {
+  const int j0 = t * BN;
+  if (j0 >= len) return 0;
+  int first, last;
+  swa_query_tiles(t, BN, BN, W, ns, len, &first, &last);
+  const int nq = last - first + 1, it0 = split * per, it1 = min(it0 + per, G * nq);
+  if (it0 >= it1) return 0;
+  const int q = it0 / nq == (it1 - 1) / nq ? first + it0 % nq : first;  // its first query tile
+  return j0 < ns && q * BN - W >= j0 + BN - 1 ? min(BN, ns - j0) : BN;
+}
+
 // bfloat16 with d = 64 or 128 runs on the tensor cores
 bool swa_tc_supported(const SwaArgs &a);
 kdn_status_t launch_swa_fwd_tc(const SwaArgs &a, cudaStream_t s);

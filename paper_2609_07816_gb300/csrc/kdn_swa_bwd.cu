@@ -296,22 +296,21 @@ __global__ void __launch_bounds__(THREADS, 1)
     const bool part = x < sp.part_blocks;
     const uint32_t acc = (wg ? TK : TV) + lanes;
     unsigned char *so = wg ? sk : sv;
-    if (ok && part) {
+    const int rows = part ? swa_split_rows(t, split, per, TILE, a.W, a.ns, a.G, len) : TILE;
+    if (ok && part && 32 * (warp & 3) < rows) {
       float *dst = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x) * (2 * TILE * D) + (wg ? 0 : TILE * D) +
                    (size_t)r * D;
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         float o[32];
-        if (N > 0) {
-          tmem_ld32(acc + c, o);
-          tmem_ld_wait<32>(o);
-        }
+        tmem_ld32(acc + c, o);  // rows > 0: the split has iterations
+        tmem_ld_wait<32>(o);
+        if (r < rows)
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<float4 *>(dst + c + e) =
-              N > 0 ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4 *>(dst + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
-    } else if (ok) {
+    } else if (ok && !part) {
       acc_to_tile<D>(acc, so, r, 0, wg ? a.scale : 1.f, j < len && N > 0, N > 0);
       fence_proxy_async();
     }

@@ -382,26 +382,35 @@ template <typename DT> __global__ void __launch_bounds__(NT) k_swa_prep(const Sw
   }
 }
 
-// dk, dv of split key tiles: their partial sums added in split order.
+// dk, dv of split key tiles: their partial sums added in split order, four channels a
+// thread.  Bound by reading the partial sums.
 template <typename DT> __global__ void __launch_bounds__(NT) k_swa_join(const SwaArgs a, const SwaSplits sp, int BN) {
-  const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x;
+  const int d4 = a.d / 4, chunks = BN * d4 / NT;  // NT divides BN d / 4
+  const int b = blockIdx.z, hk = blockIdx.y, t = blockIdx.x / chunks;
+  const int e = (blockIdx.x % chunks) * NT + threadIdx.x, row = e / d4, j = t * BN + row;
   const bool sink = t < sp.sink_tiles;
-  const int n = sink ? sp.splits_sink : sp.splits;
+  const int n = sink ? sp.splits_sink : sp.splits, per = sink ? sp.per_sink : sp.per;
   const int x0 = sink ? t * n : sp.sink_tiles * sp.splits_sink + (t - sp.sink_tiles) * n;
   const int len = swa_len(a, b);
-  const size_t one = (size_t)2 * BN * a.d;
-  const float *part = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x0) * one;
-  for (int e = threadIdx.x; e < BN * a.d; e += NT) {
-    const int j = t * BN + e / a.d;
-    if (j >= a.T) break;
-    float k = 0.f, v = 0.f;
+  const size_t half = (size_t)BN * d4;
+  const float4 *part = reinterpret_cast<const float4 *>(a.part) +
+                       (((size_t)b * a.Hk + hk) * sp.part_blocks + x0) * 2 * half + e;
+  if (j >= a.T) return;
+  float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
+  if (j < len)
+#pragma unroll 4
     for (int s = 0; s < n; ++s) {
-      k += part[s * one + e];
-      v += part[s * one + BN * a.d + e];
+      if (row >= swa_split_rows(t, s, per, BN, a.W, a.ns, a.G, len)) continue;
+      const float4 x = part[2 * s * half], y = part[(2 * s + 1) * half];
+      k.x += x.x; k.y += x.y; k.z += x.z; k.w += x.w;
+      v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
     }
-    const size_t at = (((size_t)b * a.T + j) * a.Hk + hk) * a.d + e % a.d;
-    st<DT>(a.dk, at, j < len ? k * a.scale : 0.f);
-    st<DT>(a.dv, at, j < len ? v : 0.f);
+  const size_t at = (((size_t)b * a.T + j) * a.Hk + hk) * a.d + 4 * (e % d4);
+  const float kk[4] = {k.x, k.y, k.z, k.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    st<DT>(a.dk, at + c, kk[c] * a.scale);
+    st<DT>(a.dv, at + c, vv[c]);
   }
 }
 
@@ -549,7 +558,7 @@ kdn_status_t launch_swa_prep(const SwaArgs &a, cudaStream_t s) {
 
 kdn_status_t launch_swa_join(const SwaArgs &a, const SwaSplits &sp, int BN, cudaStream_t s) {
   if (!sp.part_blocks) return KDN_OK;
-  const dim3 grid(sp.splits > 1 ? sp.tiles : sp.sink_tiles, a.Hk, a.B);
+  const dim3 grid((sp.splits > 1 ? sp.tiles : sp.sink_tiles) * (BN * a.d / 4 / NT), a.Hk, a.B);
   if (a.dtype == KDN_BF16) k_swa_join<__nv_bfloat16><<<grid, NT, 0, s>>>(a, sp, BN);
   else k_swa_join<float><<<grid, NT, 0, s>>>(a, sp, BN);
   return launched();
