@@ -9,7 +9,8 @@
 // the five of a single kernel that adds dQ with atomics.
 //   k_swa_dkv  a CTA owns 128 keys of a kv head and goes over the query tiles that see
 //              them, for every query head of the group.  S^T and dP^T have keys as rows:
-//              P^T and dS^T go back to TMEM as bf16 A operands of dV and dK.
+//              P^T and dS^T go back to TMEM as bf16 A operands of dV and dK, both in the
+//              place of dP^T, so that the next S^T is formed while P and dS are.
 //   k_swa_dq   a CTA owns 128 queries and goes over the keys that they see.
 // 256 threads do the pointwise part, each a row and 64 of its 128 columns (two threads
 // share a row), one warp loads, one thread issues the products.
@@ -28,23 +29,22 @@ template <int D> __device__ __forceinline__ void mma_d(uint32_t acc, uint64_t a,
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) umma_bf16(acc, a + step_k(kk), b + step_k(kk), id, kk > 0);
 }
-// acc += A B over the 128 columns of A in TMEM, which lie as bf16 in the first half of
-// each 64-column half of their region; B along its rows
+// acc += A B over the 128 columns of A in TMEM, which lie as bf16 in 32 columns of each
+// 64-column half of their region; B along its rows
 __device__ __forceinline__ void mma_t(uint32_t acc, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
 #pragma unroll
   for (int kk = 0; kk < TILE / 16; ++kk)
     umma_ts(acc, a + (kk >> 2) * 64 + (kk & 3) * 8, b + step_mn(kk), id, kk ? 1u : accumulate);
 }
 
-// 64 columns as bf16 into the first 32 columns of `taddr`
-__device__ __forceinline__ void store_bf16(uint32_t taddr, const float *x) {
+// 64 values as bf16 in 32 registers, and those into 32 columns
+__device__ __forceinline__ void pack64(uint32_t *u, const float *x) {
 #pragma unroll
-  for (int c = 0; c < 64; c += 32) {
-    uint32_t u[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) u[e] = pack_bf2(x[c + 2 * e], x[c + 2 * e + 1]);
-    tmem_st16u(taddr + c / 2, u);
-  }
+  for (int e = 0; e < 32; ++e) u[e] = pack_bf2(x[2 * e], x[2 * e + 1]);
+}
+__device__ __forceinline__ void store32(uint32_t taddr, const uint32_t *u) {
+  tmem_st16u(taddr, u);
+  tmem_st16u(taddr + 16, u + 16);
 }
 
 // Columns [c0, c0 + n) of a 128-row accumulator times f as bf16 into a swizzled tile
@@ -71,7 +71,8 @@ __device__ __forceinline__ void acc_to_tile(uint32_t taddr, unsigned char *tile,
 // ------------------------------------------------------------------ dK, dV
 
 constexpr int KV_STAGES = 2;  // stages of (Q, dO)
-template <int D> constexpr int KV_SMEM = (2 + 2 * KV_STAGES) * TILE_BYTES<D> + KV_STAGES * 2 * TILE * 4 + 256 + 1024;
+constexpr int ROW_STAGES = 4;  // stages of the row sums, which come by plain loads
+template <int D> constexpr int KV_SMEM = (2 + 2 * KV_STAGES) * TILE_BYTES<D> + ROW_STAGES * 2 * TILE * 4 + 256 + 1024;
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -79,17 +80,17 @@ __global__ void __launch_bounds__(THREADS, 1)
               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mg,
               const __grid_constant__ CUtensorMap mdk, const __grid_constant__ CUtensorMap mdv, const SwaArgs a,
               const SwaSplits sp) {
-  constexpr int NS = KV_STAGES, TB = TILE_BYTES<D>, SL = D / 64;
+  constexpr int NS = KV_STAGES, NR = ROW_STAGES, TB = TILE_BYTES<D>, SL = D / 64;
   extern __shared__ unsigned char smraw[];
   unsigned char *sm =
       reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
   unsigned char *sk = sm, *sv = sk + TB, *sq = sv + TB, *sg = sq + NS * TB;
   float *srow = reinterpret_cast<float *>(sg + NS * TB);  // [stage][nlse, delta][128]
-  uint64_t *bars = reinterpret_cast<uint64_t *>(srow + NS * 2 * TILE);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(srow + NR * 2 * TILE);
   uint64_t *q_full = bars, *q_empty = q_full + NS, *g_full = q_empty + NS, *g_empty = g_full + NS;
-  uint64_t *l_full = g_empty + NS, *l_empty = l_full + NS;
-  uint64_t *kv_full = l_empty + NS, *s_full = kv_full + 1, *dp_full = s_full + 1, *p_full = dp_full + 1;
-  uint64_t *ds_full = p_full + 1, *done = ds_full + 1;
+  uint64_t *clean = g_empty + NS, *l_full = clean + NS, *l_empty = l_full + NR;
+  uint64_t *kv_full = l_empty + NR, *s_full = kv_full + 1, *s_read = s_full + 1, *dp_full = s_read + 1;
+  uint64_t *p_full = dp_full + 1, *ds_full = p_full + 1, *done = ds_full + 1;
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(done + 1);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
 
@@ -110,11 +111,15 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(q_empty + i, 1);
       mbar_init(g_full + i, 1);
       mbar_init(g_empty + i, 1);
+      mbar_init(clean + i, 1);
+    }
+    for (int i = 0; i < NR; ++i) {
       mbar_init(l_full + i, 1);
       mbar_init(l_empty + i, SOFT);
     }
     mbar_init(kv_full, 1);
     mbar_init(s_full, 1);
+    mbar_init(s_read, SOFT);
     mbar_init(dp_full, 1);
     mbar_init(p_full, SOFT);
     mbar_init(ds_full, SOFT);
@@ -145,10 +150,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           tma_load_4d(sk + s * SLAB, &mk, kv_full, 64 * s, hk, j0, b);
           tma_load_4d(sv + s * SLAB, &mv, kv_full, 64 * s, hk, j0, b);
         }
-        int n = 0, qloads = 0, gloads = 0;
-        for (; n < N; ++n) {
-          const int st = n % NS, par = (n / NS - 1) & 1, it = it0 + n;
-          const int h = hk * a.G + it / nq, i0 = (first + it % nq) * TILE;
+        int qloads = 0, gloads = 0, h = hk * a.G + it0 / nq, qt = it0 % nq;
+        for (int n = 0; n < N; ++n) {
+          const int st = n % NS, par = (n / NS - 1) & 1, i0 = (first + qt) * TILE;
           if (n >= NS && !wait(q_empty + st, par)) break;
           mbar_expect_tx(q_full + st, TB);
           for (int s = 0; s < SL; ++s) tma_load_4d(sq + st * TB + s * SLAB, &mq, q_full + st, 64 * s, h, i0, b);
@@ -157,6 +161,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           mbar_expect_tx(g_full + st, TB);
           for (int s = 0; s < SL; ++s) tma_load_4d(sg + st * TB + s * SLAB, &mg, g_full + st, 64 * s, h, i0, b);
           ++gloads;
+          if (++qt == nq) { qt = 0; ++h; }
         }
         if (*wait.fail) {  // copies in flight land before the CTA leaves
           mbar_wait(kv_full, 0, kWait);
@@ -171,12 +176,11 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint64_t mq_ = desc_mn(sq), mg_ = desc_mn(sg);
         auto off = [](int st) { return (uint64_t)(st * (TB >> 4)); };
         bool ok = wait(kv_full, 0);
-        // S^T of query tile n; a ragged last tile's Q and dO have been cleared by then
+        // S^T of query tile n
         auto s_mma = [&](int n) {
           const int st = n % NS, par = (n / NS) & 1;
           if (!wait(q_full + st, par)) return false;
-          const int i0 = (first + (it0 + n) % nq) * TILE;
-          if (i0 + TILE > len && len < a.T && !wait(l_full + st, par)) return false;
+          if (len < a.T && !wait(clean + st, par)) return false;
           mma_d<D>(TS, dk, dq + off(st), id_s);
           umma_commit(s_full);
           return true;
@@ -190,39 +194,58 @@ __global__ void __launch_bounds__(THREADS, 1)
         ok = ok && s_mma(0) && dp_mma(0);
         for (int n = 0; ok && n < N; ++n) {
           const int st = n % NS;
+          if (n + 1 < N) {
+            if (!(ok = wait(s_read, n & 1))) break;
+            tc_fence_after();
+            if (!(ok = s_mma(n + 1))) break;
+          }
           if (!(ok = wait(p_full, n & 1))) break;
           tc_fence_after();
-          mma_t(TV, TS, mg_ + off(st), id_o, n > 0);
+          mma_t(TV, TP, mg_ + off(st), id_o, n > 0);
           umma_commit(g_empty + st);
-          if (n + 1 < N && !(ok = s_mma(n + 1))) break;
           if (!(ok = wait(ds_full, n & 1))) break;
           tc_fence_after();
-          mma_t(TK, TP, mq_ + off(st), id_o, n > 0);
+          mma_t(TK, TP + 32, mq_ + off(st), id_o, n > 0);
           umma_commit(n + 1 < N ? q_empty + st : done);
           if (n + 1 < N) ok = dp_mma(n + 1);
         }
       }
-    } else if (warp == 10) {  // ------------------------- row sums; ragged last tiles
+    } else if (warp == 10) {  // --------------------------------------- row sums
+      int g = it0 / max(nq, 1), qt = it0 % max(nq, 1);
       for (int n = 0; n < N; ++n) {
-        const int st = n % NS, par = (n / NS) & 1, it = it0 + n;
-        const int h = hk * a.G + it / nq, i0 = (first + it % nq) * TILE;
-        if (n >= NS && !wait.warp(l_empty + st, par ^ 1)) break;
-        const size_t row0 = ((size_t)b * a.H + h) * a.T;
+        const int st = n % NR, h = hk * a.G + g, i0 = (first + qt) * TILE;
+        const float *nl = a.nlse + ((size_t)b * a.H + h) * a.T + i0, *de = a.delta + (nl - a.nlse);
+        float x[4], y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int i = 32 * c + lane;
+          x[c] = i0 + i < len ? nl[i] : INFINITY;
+          y[c] = i0 + i < len ? de[i] : 0.f;
+        }
+        if (n >= NR && !wait.warp(l_empty + st, (n / NR - 1) & 1)) break;
         float *d = srow + st * 2 * TILE;
 #pragma unroll
-        for (int c = 0; c < TILE; c += 32) {
-          const int i = i0 + c + lane;
-          d[c + lane] = i < len ? a.nlse[row0 + i] : INFINITY;
-          d[TILE + c + lane] = i < len ? a.delta[row0 + i] : 0.f;
+        for (int c = 0; c < 4; ++c) {
+          d[32 * c + lane] = x[c];
+          d[TILE + 32 * c + lane] = y[c];
         }
-        if (i0 + TILE > len && len < a.T) {
-          if (!wait.warp(q_full + st, par) || !wait.warp(g_full + st, par)) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(l_full + st);
+        if (++qt == nq) { qt = 0; ++g; }
+      }
+    } else if (warp == 11 && len < a.T) {  // ------ a ragged last tile's Q and dO
+      int qt = it0 % max(nq, 1);
+      for (int n = 0; n < N; ++n) {
+        const int st = n % NS, par = (n / NS) & 1, i0 = (first + qt) * TILE;
+        if (!wait.warp(q_full + st, par) || !wait.warp(g_full + st, par)) break;
+        if (i0 + TILE > len) {
           zero_rows(sq + st * TB, SL, len - i0, lane);
           zero_rows(sg + st * TB, SL, len - i0, lane);
           fence_proxy_async();
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(l_full + st);
+        if (lane == 0) mbar_arrive(clean + st);
+        if (++qt == nq) qt = 0;
       }
     }
   } else {  // ----------------------------------------------------------- pointwise
@@ -233,16 +256,20 @@ __global__ void __launch_bounds__(THREADS, 1)
     const float c2 = a.scale * kLog2e;
     const float2 cc = make_float2(c2, c2);
     bool ok = true;
+    int qt = it0 % max(nq, 1);
     for (int n = 0; n < N; ++n) {
-      const int st = n % NS, i0 = (first + (it0 + n) % nq) * TILE;
+      const int st = n % NR, i0 = (first + qt) * TILE;
+      if (++qt == nq) qt = 0;
       const float *nl = srow + st * 2 * TILE + q0, *de = nl + TILE;
-      if (!(ok = wait.warp(l_full + st, (n / NS) & 1))) break;
+      if (!(ok = wait.warp(l_full + st, (n / NR) & 1))) break;
       if (!(ok = wait.warp(s_full, n & 1))) break;
       tc_fence_after();
       float p[64];
       tmem_ld32(ts, p);
       tmem_ld32(ts + 32, p + 32);
       tmem_ld_wait<64>(p);
+      tc_fence_before();
+      mbar_arrive(s_read);
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
         const float4 l4 = *reinterpret_cast<const float4 *>(nl + c);
@@ -262,16 +289,18 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int e = 0; e < 32; ++e) p[c + e] = (see >> e & 1u) ? p[c + e] : 0.f;
         }
       }
-      store_bf16(ts, p);
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(p_full);
+      uint32_t u[32];
+      pack64(u, p);
       if (!(ok = wait.warp(dp_full, n & 1))) break;
       tc_fence_after();
       float g[64];
       tmem_ld32(tp, g);
       tmem_ld32(tp + 32, g + 32);
       tmem_ld_wait<64>(g);
+      store32(tp, u);  // P^T and dS^T take the place of this thread's part of dP^T
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive(p_full);
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
         const float4 d4 = *reinterpret_cast<const float4 *>(de + c);
@@ -284,7 +313,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         g[c + 2] = z.x;
         g[c + 3] = z.y;
       }
-      store_bf16(tp, g);
+      pack64(u, g);
+      store32(tp + 32, u);
       tmem_st_wait();
       tc_fence_before();
       mbar_arrive(ds_full);
@@ -512,7 +542,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         g[c] = y.x;
         g[c + 1] = y.y;
       }
-      store_bf16(ts, g);
+      uint32_t u[32];
+      pack64(u, g);
+      store32(ts, u);
       tmem_st_wait();
       tc_fence_before();
       mbar_arrive(ds_full);
