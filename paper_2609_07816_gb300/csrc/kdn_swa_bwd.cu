@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           x[c] = i0 + i < len ? nl[i] : INFINITY;
           y[c] = i0 + i < len ? de[i] : 0.f;
         }
-        if (n >= NR && !wait.warp(l_empty + st, (n / NR - 1) & 1)) break;
+        if (n >= NR) wait.warp(l_empty + st, (n / NR - 1) & 1);
         float *d = srow + st * 2 * TILE;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -237,7 +237,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       int qt = it0 % max(nq, 1);
       for (int n = 0; n < N; ++n) {
         const int st = n % NS, par = (n / NS) & 1, i0 = (first + qt) * TILE;
-        if (!wait.warp(q_full + st, par) || !wait.warp(g_full + st, par)) break;
+        wait.warp(q_full + st, par);
+        wait.warp(g_full + st, par);
         if (i0 + TILE > len) {
           zero_rows(sq + st * TB, SL, len - i0, lane);
           zero_rows(sg + st * TB, SL, len - i0, lane);
@@ -255,14 +256,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t ts = TS + lanes + q0, tp = TP + lanes + q0;
     const float c2 = a.scale * kLog2e;
     const float2 cc = make_float2(c2, c2);
-    bool ok = true;
     int qt = it0 % max(nq, 1);
     for (int n = 0; n < N; ++n) {
       const int st = n % NR, i0 = (first + qt) * TILE;
       if (++qt == nq) qt = 0;
       const float *nl = srow + st * 2 * TILE + q0, *de = nl + TILE;
-      if (!(ok = wait.warp(l_full + st, (n / NR) & 1))) break;
-      if (!(ok = wait.warp(s_full, n & 1))) break;
+      wait.warp(l_full + st, (n / NR) & 1);
+      wait.warp(s_full, n & 1);
       tc_fence_after();
       float p[64];
       tmem_ld32(ts, p);
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       uint32_t u[32];
       pack64(u, p);
-      if (!(ok = wait.warp(dp_full, n & 1))) break;
+      wait.warp(dp_full, n & 1);
       tc_fence_after();
       float g[64];
       tmem_ld32(tp, g);
@@ -320,14 +320,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_arrive(ds_full);
       mbar_arrive(l_empty + st);
     }
-    if (ok && N > 0) ok = wait.warp(done, 0);
+    if (N > 0) wait.warp(done, 0);
     tc_fence_after();
     // threads of the first half store dV, those of the second dK
     const bool part = x < sp.part_blocks;
     const uint32_t acc = (wg ? TK : TV) + lanes;
     unsigned char *so = wg ? sk : sv;
     const int rows = part ? swa_split_rows(t, split, per, TILE, a.W, a.ns, a.G, len) : TILE;
-    if (ok && part && 32 * (warp & 3) < rows) {
+    if (part && 32 * (warp & 3) < rows) {
       float *dst = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x) * (2 * TILE * D) + (wg ? 0 : TILE * D) +
                    (size_t)r * D;
 #pragma unroll 1
@@ -340,12 +340,12 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int e = 0; e < 32; e += 4)
             *reinterpret_cast<float4 *>(dst + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
-    } else if (ok && !part) {
+    } else if (!part) {
       acc_to_tile<D>(acc, so, r, 0, wg ? a.scale : 1.f, j < len && N > 0, N > 0);
       fence_proxy_async();
     }
     named_sync(1 + wg, TILE);
-    if (r == 0 && ok && !part) {  // rows past T are not written
+    if (r == 0 && !part) {  // rows past T are not written
       for (int s = 0; s < SL; ++s) tma_store_4d(wg ? &mdk : &mdv, so + s * SLAB, 64 * s, hk, j0, b);
       bulk_commit();
       bulk_wait_all();
@@ -452,13 +452,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (ragged) {  // the last tile's keys past the length
         const int m = N - 1;
-        if (wait.warp(k_full + m % NK, (m / NK) & 1) && wait.warp(v_full + m % NV, (m / NV) & 1)) {
-          zero_rows(sk + m % NK * TB, SL, len % TILE, lane);
-          zero_rows(sv + m % NV * TB, SL, len % TILE, lane);
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(clean);
-        }
+        wait.warp(k_full + m % NK, (m / NK) & 1);
+        wait.warp(v_full + m % NV, (m / NV) & 1);
+        zero_rows(sk + m % NK * TB, SL, len % TILE, lane);
+        zero_rows(sv + m % NV * TB, SL, len % TILE, lane);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(clean);
       }
     } else if (warp == 9 && N > 0) {  // ---------------------------------- products
       if (elect_one()) {
@@ -504,11 +504,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     const size_t row = ((size_t)b * a.H + h) * a.T + i;
     const float nl = i < len ? -a.nlse[row] : -INFINITY, de = i < len ? -a.delta[row] : 0.f;
     const float2 cc = make_float2(c2, c2), nn = make_float2(nl, nl), dd = make_float2(de, de);
-    bool ok = true;
     for (int n = 0; n < N; ++n) {
       const int j0 = kt.at(n) * TILE;
       const uint32_t ts = tb + (n & 1) * 128 + lanes + k0;
-      if (!(ok = wait.warp(s_full + (n & 1), (n >> 1) & 1))) break;
+      wait.warp(s_full + (n & 1), (n >> 1) & 1);
       tc_fence_after();
       float p[64];
       tmem_ld32(ts, p);
@@ -528,7 +527,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int e = 0; e < 32; ++e) p[c + e] = (see >> e & 1u) ? p[c + e] : 0.f;
         }
       }
-      if (!(ok = wait.warp(dp_full, n & 1))) break;
+      wait.warp(dp_full, n & 1);
       tc_fence_after();
       float g[64];
       tmem_ld32(tp, g);
@@ -549,15 +548,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       tc_fence_before();
       mbar_arrive(ds_full);
     }
-    if (ok && N > 0) ok = wait.warp(done, 0);
+    if (N > 0) wait.warp(done, 0);
     tc_fence_after();
     // two threads a query, half of the channels each, through the queries' place in shared memory
-    if (ok) {
-      acc_to_tile<D / 2>(TQ + lanes, sq, r, wg * (D / 2), a.scale, i < len, N > 0);
-      fence_proxy_async();
-    }
+    acc_to_tile<D / 2>(TQ + lanes, sq, r, wg * (D / 2), a.scale, i < len, N > 0);
+    fence_proxy_async();
     named_sync(1, SOFT);
-    if (tid == 0 && ok) {  // rows past T are not written
+    if (tid == 0) {  // rows past T are not written
       for (int s = 0; s < SL; ++s) tma_store_4d(&mdq, sq + s * SLAB, 64 * s, h, i0, b);
       bulk_commit();
       bulk_wait_all();

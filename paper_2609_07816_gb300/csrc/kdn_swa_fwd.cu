@@ -118,12 +118,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (len < a.T && kt.at(N - 1) * TILE + TILE > len) {  // the last tile's V past the length
         const int st = (N - 1) % NS;
-        if (wait.warp(v_full + st, ((N - 1) / NS) & 1)) {
-          zero_rows(sv + st * TB, SL, len % TILE, lane);
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(v_clean);
-        }
+        wait.warp(v_full + st, ((N - 1) / NS) & 1);
+        zero_rows(sv + st * TB, SL, len % TILE, lane);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(v_clean);
       }
     } else if (warp == 9 && N > 0) {  // ---------------------------------- products
       if (elect_one()) {
@@ -184,11 +183,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     const Half hx = x ? half[1] : half[0];
     float ref = -INFINITY, l = 0.f;
     int k = 0;
-    bool ok = true;
     for (int n = 0; n < N; ++n) {
       const int t = kt.at(n), j0 = t * TILE;
       if (!hx.needs(t)) continue;
-      if (!(ok = wait.warp(s_full + x, k & 1))) break;
+      wait.warp(s_full + x, k & 1);
       tc_fence_after();
       float s[TILE];
 #pragma unroll
@@ -252,10 +250,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_arrive(p_full + x);
       ++k;
     }
-    if (ok && k > 0) ok = wait.warp(o_full + x, 0);
+    if (k > 0) wait.warp(o_full + x, 0);
     // o through shared memory (this accumulator's queries are no longer needed there)
     unsigned char *so = sq + x * TB;
-    if (ok && r0 < a.T) {
+    if (r0 < a.T) {
       const bool live = i < len;
       const float inv = live ? 1.f / l : 0.f;
       tc_fence_after();
@@ -280,7 +278,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       fence_proxy_async();
     }
     named_sync(1 + x, TILE);
-    if (r == 0 && ok && r0 < a.T) {  // rows past T are not written
+    if (r == 0 && r0 < a.T) {  // rows past T are not written
       for (int s = 0; s < SL; ++s) tma_store_4d(&mo, so + s * SLAB, 64 * s, h, r0, b);
       bulk_commit();
       bulk_wait_all();

@@ -23,16 +23,28 @@ SwaSplits swa_splits(const SwaArgs &a, int BM, int BN) {
   const long long reach = (long long)a.W + BN - 2;  // last query of a window tile, from its first key
   const int nq = (int)(reach / BM + 1 < qtiles ? reach / BM + 1 : qtiles);
   const int iters = a.G * nq, iters_sink = a.G * qtiles;
-  // Split a tile's iterations when there are fewer tiles than SMs.  A split pays for
-  // writing and re-reading 8 BN d bytes of partial sums, about three iterations' time.
-  const long long whole = (long long)a.B * a.Hk * p.tiles;
-  int want = whole >= 152 ? 1 : cdiv(152, whole > 0 ? whole : 1);
-  if (want > iters / 4) want = iters / 4 > 0 ? iters / 4 : 1;
-  p.per = cdiv(iters, want);
+  // Iterations of a split, where whole tiles would be less than two waves of one CTA an
+  // SM: the length that ends soonest, each wave taking its longest split and a fixed part
+  // (first loads, last stores; about two iterations, and two more where partial sums are
+  // written and joined).  Many more splits than SMs would be bound by those sums.  Splits
+  // of a sink tile have the length of the others, or (none split) at most twice it.
+  const long long heads = (long long)a.B * a.Hk;
+  long long whole = 0;
+  double best = 0;
+  for (int n = 1; n <= 8 && (n == 1 || iters / n >= 2); ++n) {
+    const int per = cdiv(iters, n), per_sink = n == 1 && iters_sink <= 2 * iters ? iters_sink : per;
+    const long long blocks = (long long)p.sink_tiles * cdiv(iters_sink, per_sink) +
+                             (long long)(p.tiles - p.sink_tiles) * cdiv(iters, per);
+    const int longest = p.sink_tiles && per_sink > per ? per_sink : per;
+    if (n == 1) whole = heads * blocks;
+    const double cost = (double)((heads * blocks + 151) / 152) * (longest + (n == 1 ? 2 : 4));
+    if (n == 1 ? true : whole < 2 * 152 && cost < 0.95 * best) {
+      best = cost;
+      p.per = per;
+      p.per_sink = per_sink;
+    }
+  }
   p.splits = cdiv(iters, p.per);
-  // The sinks' tiles are seen by all later queries: cut to the length of the others,
-  // unless that is within twice theirs.
-  p.per_sink = (p.splits == 1 && iters_sink <= 2 * iters) ? iters_sink : p.per;
   p.splits_sink = cdiv(iters_sink, p.per_sink);
   p.blocks = p.sink_tiles * p.splits_sink + (p.tiles - p.sink_tiles) * p.splits;
   p.part_blocks = p.splits > 1 ? p.blocks : p.splits_sink > 1 ? p.sink_tiles * p.splits_sink : 0;
@@ -353,32 +365,36 @@ __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSp
   }
 }
 
-// delta_i = sum_d o_id dO_id, and lse in log2 units: one warp a row, rows in memory
-// order.  Rows past the length (and rows whose lse says that they see nothing) get
-// +inf, so that their weights are exp2(-inf) = 0.  Reads 2 d elements a row: bandwidth.
-template <typename DT> __global__ void __launch_bounds__(NT) k_swa_prep(const SwaArgs a) {
-  const size_t row = (size_t)blockIdx.x * (NT / 32) + threadIdx.x / 32, rows = (size_t)a.B * a.T * a.H;
-  const int lane = threadIdx.x % 32;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-  if (row >= rows) return;
-  const int h = (int)(row % a.H);
-  const size_t bt = row / a.H;
-  const int t = (int)(bt % a.T), b = (int)(bt / a.T);
-  const size_t out = ((size_t)b * a.H + h) * a.T + t;
-  if (t >= swa_len(a, b)) {
-    if (lane == 0) { a.nlse[out] = INFINITY; a.delta[out] = 0.f; }
-    return;
+// delta_i = sum_d o_id dO_id, and lse in log2 units.  Rows past the length get +inf, so
+// that their weights are exp2(-inf) = 0.  LPR lanes share a row, 16 bytes each; a CTA
+// takes 4 NT / LPR tokens of a head, so that its row sums leave in one run of memory.
+// Reads 2 d elements a row: bandwidth.
+template <typename DT, int LPR> __global__ void __launch_bounds__(NT) k_swa_prep(const SwaArgs a) {
+  constexpr int V = 16 / (int)sizeof(DT), RPP = NT / LPR, PASSES = 4;
+  const int b = blockIdx.z, h = blockIdx.y, len = swa_len(a, b);
+  const int ln = threadIdx.x % LPR, t0 = blockIdx.x * RPP * PASSES + threadIdx.x / LPR;
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *a.status = 0;
+  uint4 x[PASSES], y[PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int t = t0 + p * RPP;
+    const size_t at = (((size_t)b * a.T + t) * a.H + h) * LPR + ln;
+    x[p] = t < len ? static_cast<const uint4 *>(a.o)[at] : make_uint4(0, 0, 0, 0);
+    y[p] = t < len ? static_cast<const uint4 *>(a.dO)[at] : make_uint4(0, 0, 0, 0);
   }
-  float x = 0.f;
-  for (int c = 2 * lane; c < a.d; c += 64) {
-    x = fmaf(ld<DT>(a.o, row * a.d + c), ld<DT>(a.dO, row * a.d + c), x);
-    x = fmaf(ld<DT>(a.o, row * a.d + c + 1), ld<DT>(a.dO, row * a.d + c + 1), x);
-  }
-  x = warp_sum(x);
-  if (lane == 0) {
-    const float l = a.lse[out];
-    a.nlse[out] = l == -INFINITY ? INFINITY : l * kLog2e;
-    a.delta[out] = x;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int t = t0 + p * RPP;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) s = fmaf(ld<DT>(&x[p], e), ld<DT>(&y[p], e), s);
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (ln == 0 && t < a.T) {
+      const size_t out = ((size_t)b * a.H + h) * a.T + t;
+      a.nlse[out] = t < len ? a.lse[out] * kLog2e : INFINITY;
+      a.delta[out] = s;
+    }
   }
 }
 
@@ -549,10 +565,17 @@ kdn_status_t launch_swa_decode_general(const SwaArgs &a, void *kc, void *vc, con
 }
 
 kdn_status_t launch_swa_prep(const SwaArgs &a, cudaStream_t s) {
-  const size_t rows = (size_t)a.B * a.T * a.H;
-  const unsigned grid = (unsigned)((rows + NT / 32 - 1) / (NT / 32));
-  if (a.dtype == KDN_BF16) k_swa_prep<__nv_bfloat16><<<grid, NT, 0, s>>>(a);
-  else k_swa_prep<float><<<grid, NT, 0, s>>>(a);
+  const int lpr = a.d * (a.dtype == KDN_BF16 ? 2 : 4) / 16, rows = 4 * NT / lpr;
+  const dim3 grid((a.T + rows - 1) / rows, a.H, a.B);
+  if (a.dtype == KDN_BF16) {
+    if (lpr == 16) k_swa_prep<__nv_bfloat16, 16><<<grid, NT, 0, s>>>(a);
+    else if (lpr == 8) k_swa_prep<__nv_bfloat16, 8><<<grid, NT, 0, s>>>(a);
+    else k_swa_prep<__nv_bfloat16, 4><<<grid, NT, 0, s>>>(a);
+  } else {
+    if (lpr == 32) k_swa_prep<float, 32><<<grid, NT, 0, s>>>(a);
+    else if (lpr == 16) k_swa_prep<float, 16><<<grid, NT, 0, s>>>(a);
+    else k_swa_prep<float, 8><<<grid, NT, 0, s>>>(a);
+  }
   return launched();
 }
 

@@ -133,29 +133,28 @@ __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-// A bounded wait that gives up for the whole CTA: the first role whose wait runs out
-// raises `fail` (shared memory) and records the timeout; the others see it and leave.
-__device__ __forceinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *fail, unsigned *status) {
-  for (uint32_t i = 0; i < kWait; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (i > 256) {
-      if (*fail) return false;
-      __nanosleep(64);
-    }
-  }
-  *fail = 1;
-  atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
-  return false;
-}
+// A bounded wait that gives up for the whole CTA: the first thread whose wait runs out
+// raises `fail` (shared memory) and records the timeout; from then on no wait of the CTA
+// lasts.  Threads that must stay together go on regardless (what they compute is invalid
+// and the status says so); the loading and the issuing thread leave their loops.
 struct Waiter {
   volatile int *fail;
   unsigned *status;
   __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
-    return mbar_try_wait(bar, parity) || mbar_try_wait(bar, parity) || wait_slow(bar, parity, fail, status);
+    if (mbar_try_wait(bar, parity)) return true;
+    for (uint32_t i = 0; i < kWait; ++i) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if (*fail) return false;
+      if (i > 256) __nanosleep(64);
+    }
+    *fail = 1;
+    atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
+    return false;
   }
-  // the same answer for all lanes of a warp
-  __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
-    return __all_sync(0xffffffffu, (*this)(bar, parity));
+  // by all lanes of a warp, which go on together
+  __device__ __forceinline__ void warp(uint64_t *bar, uint32_t parity) const {
+    (*this)(bar, parity);
+    __syncwarp();
   }
 };
 
