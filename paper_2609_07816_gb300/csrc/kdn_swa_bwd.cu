@@ -21,6 +21,10 @@ namespace {
 
 using namespace swa;
 
+// Barrier of the 128 (or 256) threads that share `id`.
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 constexpr int THREADS = 384, SOFT = 256;
 template <int D> constexpr int TILE_BYTES = D / 64 * SLAB;
 

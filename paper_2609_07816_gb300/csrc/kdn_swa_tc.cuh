@@ -128,11 +128,6 @@ __device__ __forceinline__ uint32_t key_bits(int hi, int W, int sinks) {
   return low_bits(hi + 1) & (~low_bits(hi - W + 1) | low_bits(sinks));
 }
 
-// Barrier of the 128 (or 256) threads that share `id`.
-__device__ __forceinline__ void named_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
 // A bounded wait that gives up for the whole CTA: the first thread whose wait runs out
 // raises `fail` (shared memory) and records the timeout; from then on no wait of the CTA
 // lasts.  Threads that must stay together go on regardless (what they compute is invalid
@@ -157,6 +152,87 @@ struct Waiter {
     __syncwarp();
   }
 };
+
+// 32 consecutive columns of a row times f as bf16 (zeros where the row is not live).
+// wide: the row is 32-byte aligned, which takes half as many stores.
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *dst, const float *x, float f, bool live, bool wide) {
+  uint32_t u[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) u[e] = live ? pack_bf2(x[2 * e] * f, x[2 * e + 1] * f) : 0u;
+  if (wide) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * e), "r"(u[e]),
+                   "r"(u[e + 1]), "r"(u[e + 2]), "r"(u[e + 3]), "r"(u[e + 4]), "r"(u[e + 5]), "r"(u[e + 6]),
+                   "r"(u[e + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<uint4 *>(dst + 2 * e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+  }
+}
+__device__ __forceinline__ bool aligned32(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
+
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^s < d <= 2^(s+1) and
+// m = ceil(2^(32+s) / d), the excess m d - 2^(32+s) is below d, and n times it below 2^(32+s).
+struct FastDiv {
+  uint32_t m, s;  // m = 0: d = 1
+  explicit FastDiv(uint32_t d) : m(0), s(0) {
+    if (d == 1) return;
+    while ((2ull << s) < d) ++s;
+    m = (uint32_t)(((1ull << (32 + s)) + d - 1) / d);
+  }
+  __device__ __forceinline__ int div(int n) const { return m ? (int)(__umulhi((uint32_t)n, m) >> s) : n; }
+};
+
+// The work items of a persistent CTA.  Its first is blockIdx.x; the loading warp takes
+// the others from a counter in global memory (zero at launch), in order, as it comes to
+// them, and hands each to the CTA's other warps through a ring in shared memory.
+constexpr int kRing = 4;
+struct ItemRing {
+  uint64_t *full, *empty;  // [kRing]; empty: one arrival a consuming warp
+  volatile int *slot;      // [kRing]
+};
+struct ItemSource {  // the loading warp
+  const ItemRing &ring;
+  const Waiter &wait;
+  unsigned *counter;
+  int total, n = 0, ahead = 0;
+  __device__ __forceinline__ ItemSource(const ItemRing &r, const Waiter &w, unsigned *c, int items)
+      : ring(r), wait(w), counter(c), total(items) {}
+  __device__ __forceinline__ int next() {  // by all lanes; -1: no more
+    int item = 0;
+    if (threadIdx.x % 32 == 0) {
+      item = n == 0 ? (int)blockIdx.x : ahead;
+      if (item >= total) item = -1;
+      // the next one's number arrives while this one is loaded
+      else if ((ahead = (int)(gridDim.x + atomicAdd(counter, 1u))) < 0) ahead = total;
+      const int s = n % kRing;
+      if (n >= kRing && !wait(ring.empty + s, (n / kRing - 1) & 1)) item = -1;
+      ring.slot[s] = item;
+      mbar_arrive(ring.full + s);
+    }
+    ++n;
+    return __shfl_sync(0xffffffffu, item, 0);
+  }
+};
+struct ItemSink {  // a warp that works on them
+  const ItemRing &ring;
+  const Waiter &wait;
+  int n = 0;
+  __device__ __forceinline__ ItemSink(const ItemRing &r, const Waiter &w) : ring(r), wait(w) {}
+  __device__ __forceinline__ int next() {  // by all lanes; -1: no more
+    const int s = n % kRing;
+    const bool ok = wait(ring.full + s, (n / kRing) & 1);
+    const int item = __shfl_sync(0xffffffffu, ok ? ring.slot[s] : -1, 0);
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) mbar_arrive(ring.empty + s);
+    ++n;
+    return item;
+  }
+};
+constexpr int kCtas = 152;  // one persistent CTA an SM
 
 // Rows [first, 128) of a tile of `slabs` slabs set to zero by one warp: tokens past a
 // sequence's length hold anything, and a weight of zero does not hide a NaN.
