@@ -163,7 +163,8 @@ kdn_status_t kdn_swa_decode_step(const kdn_swa_desc_t *desc, const void *q, cons
   if (!has_work(a)) return KDN_OK;
   if (!ptrs_ok({q, k, v, kc, vc, pos, o})) return KDN_ERR_INVALID_ARG;
   a.q = q; a.k = k; a.v = v; a.o = o;
-  return launch_swa_decode_general(a, kc, vc, pos, static_cast<cudaStream_t>(stream));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return swa_tc_supported(a) ? launch_swa_decode_tc(a, kc, vc, pos, s) : launch_swa_decode_general(a, kc, vc, pos, s);
 }
 
 kdn_status_t kdn_add_rmsnorm_fwd(const kdn_norm_desc_t *desc, const void *x, const void *res, const void *w, void *y,

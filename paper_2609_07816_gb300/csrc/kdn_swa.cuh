@@ -93,6 +93,7 @@ __device__ __forceinline__ int swa_split_rows(int t, int split, int per, int BN,
 bool swa_tc_supported(const SwaArgs &a);
 kdn_status_t launch_swa_fwd_tc(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_tc(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
+kdn_status_t launch_swa_decode_tc(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s);
 constexpr int kSwaTcTile = 128;  // query and key tile of the tensor-core kernels
 kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
