@@ -142,13 +142,13 @@ __global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm(const NormArgs a) {
       // an all-zero block has scale 1; so has one whose magnitudes are not finite (its
       // elements are NaN: a row with an infinity or a NaN has no finite norm)
       const bool ok = big > 0.f && big < INFINITY;
-      const float scale = ok ? big / kF8Max : 1.f;
+      const float scale = ok ? big / kF8Max : 1.f, inv = 1.f / scale;
       if (c < nv) {
         unsigned char q[V];
 #pragma unroll
         for (int e = 0; e < V; e += 2) {
           const __nv_fp8x2_storage_t p = __nv_cvt_float2_to_fp8x2(
-              make_float2(h[i][e] / scale, h[i][e + 1] / scale), __NV_SATFINITE, __NV_E4M3);
+              make_float2(h[i][e] * inv, h[i][e + 1] * inv), __NV_SATFINITE, __NV_E4M3);
           q[e] = (unsigned char)(p & 0xff);
           q[e + 1] = (unsigned char)(p >> 8);
         }
@@ -161,63 +161,87 @@ __global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm(const NormArgs a) {
 }
 
 // Rows are dealt out to the CTAs in turn; dw stays in registers across a CTA's rows
-// and leaves as one float32 row of partial sums a CTA.  The next row's loads are in
-// flight while the current one is reduced.
-template <typename DT, int TPR, int EPT>
-__global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm_bwd(const NormArgs a) {
-  constexpr int V = EV<DT>, NV = EPT / V, RPC = CTA<TPR> / TPR;
+// and leaves as one float32 row of partial sums a CTA.  A row is kept as it was loaded
+// (unpacked twice) so that the next one's loads can be in flight from the start of it.
+//
+// WARP: a row a warp, four of them a CTA (up to 512 columns, EPT 8 or 16).  Otherwise a
+// CTA a row, with as many threads as it has groups of EPT = 8 elements (16 beyond
+// 8192, without the early loads, for which 64 registers do not suffice): no registers
+// idle, and 1024 threads an SM whatever the width.  5.4 TB/s at 32768 x 2048 (99 us, the
+// join of dw included); 128 threads of 16 elements each, without early loads: 3.4 TB/s.
+template <typename DT, int EPT, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : 1024, WARP ? 4 : 1) k_add_rmsnorm_bwd(const NormArgs a) {
+  constexpr int V = EV<DT>, NV = EPT / V;
+  constexpr bool AHEAD = WARP || EPT == 8;
   __shared__ float red[2][32];
-  __shared__ __align__(16) float s_dw[RPC > 1 ? RPC * 32 * EPT : 1];
-  const int ln = threadIdx.x % TPR, sub = threadIdx.x / TPR, nv = a.D / V;
-  const uint4 *w = static_cast<const uint4 *>(a.w);
+  __shared__ __align__(16) float s_dw[WARP ? 4 * 32 * EPT : 1];
+  const int TPR = WARP ? 32 : blockDim.x, RPC = WARP ? 4 : 1;
+  const int ln = WARP ? threadIdx.x % 32 : threadIdx.x, sub = WARP ? threadIdx.x / 32 : 0, nv = a.D / V;
   const uint4 zero = make_uint4(0, 0, 0, 0);
   float dw[NV][V] = {};
-  uint4 uh[NV], uy[NV], ud[NV];
-  auto load = [&](long long row) {
+  uint4 w[NV];
+  struct Row {
+    uint4 h[NV], y[NV], d[NV];
+    float rstd;
+  };
+  Row cur, next;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) w[i] = i * TPR + ln < nv ? static_cast<const uint4 *>(a.w)[i * TPR + ln] : zero;
+  auto load = [&](Row &r, long long row) {
+    const bool in = row < a.rows;
+    r.rstd = in ? a.rstd_in[row] : 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = i * TPR + ln;
-      const bool ok = row < a.rows && c < nv;
-      uh[i] = ok ? static_cast<const uint4 *>(a.hin)[row * nv + c] : zero;
-      uy[i] = ok ? static_cast<const uint4 *>(a.dy)[row * nv + c] : zero;
-      ud[i] = ok && a.dh ? static_cast<const uint4 *>(a.dh)[row * nv + c] : zero;
+      const bool ok = in && c < nv;
+      r.h[i] = ok ? static_cast<const uint4 *>(a.hin)[row * nv + c] : zero;
+      r.y[i] = ok ? static_cast<const uint4 *>(a.dy)[row * nv + c] : zero;
+      r.d[i] = ok && a.dh ? static_cast<const uint4 *>(a.dh)[row * nv + c] : zero;
     }
   };
   const long long step = (long long)gridDim.x * RPC;
   long long row = (long long)blockIdx.x * RPC + sub;
-  load(row);
-  int par = 0;
-  for (; row < a.rows; row += step, par ^= 1) {
-    const float rstd = a.rstd_in[row];
-    float xh[NV][V], g[NV][V], dh[NV][V], dot = 0.f;
+  load(cur, row);
+  for (int par = 0; row < a.rows; row += step, par ^= 1) {
+    if (AHEAD) load(next, row + step);
+    float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = i * TPR + ln;
-      float t[V];
-      unpack<DT>(uh[i], xh[i]);
-      unpack<DT>(uy[i], g[i]);
-      unpack<DT>(ud[i], dh[i]);
-      unpack<DT>(c < nv ? w[c] : zero, t);
+      float xh[V], g[V], t[V];
+      unpack<DT>(cur.h[i], xh);
+      unpack<DT>(cur.y[i], g);
+      unpack<DT>(w[i], t);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        xh[i][e] *= rstd;
-        dw[i][e] = fmaf(g[i][e], xh[i][e], dw[i][e]);
-        g[i][e] *= t[e];
-        dot = fmaf(g[i][e], xh[i][e], dot);
+        xh[e] *= cur.rstd;
+        dw[i][e] = fmaf(g[e], xh[e], dw[i][e]);
+        dot = fmaf(g[e] * t[e], xh[e], dot);
       }
     }
-    load(row + step);
-    dot = row_reduce<TPR, false>(dot, red[par]) / (float)a.D;
+    dot = warp_sum(dot);
+    if constexpr (!WARP) {  // two rows' sums have their own places: one barrier a row
+      if (threadIdx.x % 32 == 0) red[par][threadIdx.x / 32] = dot;
+      __syncthreads();
+      dot = warp_sum(threadIdx.x % 32 < blockDim.x / 32 ? red[par][threadIdx.x % 32] : 0.f);
+    }
+    dot = dot / (float)a.D * cur.rstd;
     uint4 *o = static_cast<uint4 *>(a.dx) + row * nv;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      float h[V], g[V], t[V], d[V];
+      unpack<DT>(cur.h[i], h);
+      unpack<DT>(cur.y[i], g);
+      unpack<DT>(w[i], t);
+      unpack<DT>(cur.d[i], d);
 #pragma unroll
-      for (int e = 0; e < V; ++e) dh[i][e] = fmaf(rstd, fmaf(-dot, xh[i][e], g[i][e]), dh[i][e]);
-      if (i * TPR + ln < nv) o[i * TPR + ln] = pack<DT>(dh[i]);
+      for (int e = 0; e < V; ++e) d[e] = fmaf(cur.rstd, fmaf(-dot, h[e], g[e] * t[e]), d[e]);
+      if (i * TPR + ln < nv) o[i * TPR + ln] = pack<DT>(d);
     }
+    if (AHEAD) cur = next;
+    else load(cur, row + step);
   }
   float *part = a.part + (size_t)blockIdx.x * a.D;
-  if constexpr (RPC == 1) {
+  if constexpr (!WARP) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = i * TPR + ln;
@@ -229,12 +253,12 @@ __global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm_bwd(const NormArgs a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < V; ++e) s_dw[sub * 32 * EPT + (i * TPR + ln) * V + e] = dw[i][e];
+      for (int e = 0; e < V; ++e) s_dw[sub * 32 * EPT + (i * 32 + ln) * V + e] = dw[i][e];
     __syncthreads();
-    for (int c = threadIdx.x; c < a.D; c += CTA<TPR>) {
+    for (int c = threadIdx.x; c < a.D; c += 128) {
       float x = 0.f;
 #pragma unroll
-      for (int r = 0; r < RPC; ++r) x += s_dw[r * 32 * EPT + c];
+      for (int r = 0; r < 4; ++r) x += s_dw[r * 32 * EPT + c];
       part[c] = x;
     }
   }
@@ -260,13 +284,16 @@ __global__ void __launch_bounds__(1024) k_rmsnorm_dw(const float *part, int n, i
 kdn_status_t launched() { return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA; }
 
 // Threads a row and elements a thread: a warp a row up to 1024 columns (no barrier),
-// else 128 threads (up to 4096) or 512.
+// else 128 threads (up to 4096) or 512.  Elements past a row are idle registers, so
+// the steps are small: 2304 columns with 32 elements a thread in place of 24 took half
+// as long again with an 8-bit output.
 template <int TPR, int EPT> struct Shape { static constexpr int tpr = TPR, ept = EPT; };
 template <typename F> kdn_status_t by_shape(int D, F f) {
   if (D <= 256) return f(Shape<32, 8>{});
   if (D <= 512) return f(Shape<32, 16>{});
   if (D <= 1024) return f(Shape<32, 32>{});
-  if (D <= 2048) return f(Shape<128, 16>{});
+  if (D <= 128 * 16) return f(Shape<128, 16>{});
+  if (D <= 128 * 24) return f(Shape<128, 24>{});
   if (D <= 4096) return f(Shape<128, 32>{});
   if (D <= 8192) return f(Shape<512, 16>{});
   return f(Shape<512, 32>{});
@@ -280,15 +307,21 @@ template <typename DT, int F8> kdn_status_t fwd_t(const NormArgs &a, cudaStream_
   });
 }
 
+// Threads of the backward's CTA: four rows of a warp, or a row with EPT elements a thread.
+int bwd_threads(int D) {
+  if (D <= 512) return 128;
+  const int ept = D <= 8192 ? 8 : 16;
+  return ((D + ept - 1) / ept + 31) / 32 * 32;
+}
+
 template <typename DT> kdn_status_t bwd_t(const NormArgs &a, cudaStream_t s) {
-  const int n = rmsnorm_bwd_blocks(a.rows, a.D);
+  const int n = rmsnorm_bwd_blocks(a.rows, a.D), nt = bwd_threads(a.D);
   if (n) {
-    const kdn_status_t st = by_shape(a.D, [&](auto sh) {
-      constexpr int TPR = decltype(sh)::tpr, EPT = decltype(sh)::ept;
-      k_add_rmsnorm_bwd<DT, TPR, EPT><<<n, CTA<TPR>, 0, s>>>(a);
-      return launched();
-    });
-    if (st != KDN_OK) return st;
+    if (a.D <= 256) k_add_rmsnorm_bwd<DT, 8, true><<<n, nt, 0, s>>>(a);
+    else if (a.D <= 512) k_add_rmsnorm_bwd<DT, 16, true><<<n, nt, 0, s>>>(a);
+    else if (a.D <= 8192) k_add_rmsnorm_bwd<DT, 8, false><<<n, nt, 0, s>>>(a);
+    else k_add_rmsnorm_bwd<DT, 16, false><<<n, nt, 0, s>>>(a);
+    if (launched() != KDN_OK) return KDN_ERR_CUDA;
   }
   k_rmsnorm_dw<<<(a.D + 31) / 32, 1024, 0, s>>>(a.part, n, a.D, a.dw);
   return launched();
@@ -296,9 +329,9 @@ template <typename DT> kdn_status_t bwd_t(const NormArgs &a, cudaStream_t s) {
 
 }  // namespace
 
-// CTAs of the backward: enough to fill the GPU, each with its own row of partial sums.
+// CTAs of the backward: those that are resident at once, each with its own row of partial sums.
 int rmsnorm_bwd_blocks(long long rows, int D) {
-  const long long rpc = D <= 1024 ? 8 : 1, full = 152LL * (D <= 1024 ? 4 : D <= 4096 ? 5 : 2);
+  const long long rpc = D <= 512 ? 4 : 1, full = 152LL * (D <= 512 ? 4 : 1024 / bwd_threads(D));
   const long long n = (rows + rpc - 1) / rpc;
   return (int)(n < full ? n : full);
 }

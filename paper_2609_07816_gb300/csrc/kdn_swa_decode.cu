@@ -16,6 +16,7 @@
 // The new token's row is taken from the inputs wherever it is needed and written into
 // its slot by one CTA of the group: no CTA reads the slot that another one writes.
 #include <cooperative_groups.h>
+#include <math.h>
 
 #include "kdn_swa.cuh"
 
@@ -265,10 +266,22 @@ __global__ void __launch_bounds__(NT, 2)
 template <int D>
 kdn_status_t launch(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
   const int head_blocks = (a.G + HEADS - 1) / HEADS;
-  // CTAs of a cluster: enough for two CTAs an SM, each with two chunks a warp at least
-  const long long pairs = (long long)a.B * a.Hk * head_blocks, slots = (long long)a.W + a.ns;
+  // CTAs of a cluster, by what a step costs with C of them: each wave of 304 CTAs (two an
+  // SM) about 8 us of start and end, 10.5 in a cluster, 17 in one of more than 8; and the
+  // bytes, at 68 GB/s a CTA or 6.8 TB/s together.  Measured at d = 128, 2052 slots: one
+  // sequence of 16 heads 22.5, 16.4, 14.3, 12.3, 18.4 us with C = 1, 2, 4, 8, 16; 64 x 4
+  // pairs 58, 64, 68, 78, 140 us; 1 pair of 32768 slots 248, 131, 72, 41, 27 us.
+  const double pairs = (double)a.B * a.Hk * head_blocks, bytes = 4.0 * D * ((double)a.W + a.ns);
   int C = 1;
-  while (C < 16 && pairs * C < 2 * 152 && slots > (long long)C * WARPS * KEYS<D> * 2) C *= 2;
+  double best = 0;
+  for (int c = 1; c <= 16; c *= 2) {
+    const double rate = bytes / c / 68e3, all = pairs * bytes / 6.8e6;
+    const double cost = ceil(pairs * c / 304) * (c == 1 ? 8 : c <= 8 ? 10.5 : 17) + (rate > all ? rate : all);
+    if (c == 1 || cost < best) {
+      best = cost;
+      C = c;
+    }
+  }
   auto kernel = k_swa_decode_tc<D>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess ||
       cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
