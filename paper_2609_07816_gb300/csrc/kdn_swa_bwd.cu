@@ -55,7 +55,7 @@ __device__ __forceinline__ void store32(uint32_t taddr, const uint32_t *u) {
 template <int N>
 __device__ __forceinline__ void acc_to_tile(uint32_t taddr, unsigned char *tile, int r, int c0, float f, bool live,
                                             bool written) {
-#pragma unroll 1
+#pragma unroll
   for (int c = c0; c < c0 + N; c += 32) {
     float o[32];
     if (written) {
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t *bars = reinterpret_cast<uint64_t *>(srow + NR * 2 * TILE);
   uint64_t *q_full = bars, *q_empty = q_full + NS, *g_full = q_empty + NS, *g_empty = g_full + NS;
   uint64_t *clean = g_empty + NS, *l_full = clean + NS, *l_empty = l_full + NR;
-  uint64_t *kv_full = l_empty + NR, *s_full = kv_full + 1, *s_read = s_full + 1, *dp_full = s_read + 1;
+  uint64_t *kv_full = l_empty + NR, *s_full = kv_full + 2, *s_read = s_full + 1, *dp_full = s_read + 1;
   uint64_t *p_full = dp_full + 1, *ds_full = p_full + 1, *done = ds_full + 1;
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(done + 1);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
@@ -109,7 +109,22 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (j0 < len) swa_query_tiles(t, TILE, TILE, a.W, a.ns, len, &first, &last);
   const int nq = last - first + 1, it0 = split * per, N = max(0, min(per, a.G * nq - it0));
 
-  if (tid == 0) {
+  // the loading thread: K, V and the first stages are on their way before the CTA meets
+  int loads = 0, load_h = hk * a.G, load_q = 0;
+  auto load_q_tile = [&](int n) {
+    const int st = n % NS;
+    mbar_expect_tx(q_full + st, TB);
+    for (int s = 0; s < SL; ++s)
+      tma_load_4d(sq + st * TB + s * SLAB, &mq, q_full + st, 64 * s, load_h, (first + load_q) * TILE, b);
+  };
+  auto load_g_tile = [&](int n) {
+    const int st = n % NS;
+    mbar_expect_tx(g_full + st, TB);
+    for (int s = 0; s < SL; ++s)
+      tma_load_4d(sg + st * TB + s * SLAB, &mg, g_full + st, 64 * s, load_h, (first + load_q) * TILE, b);
+    if (++load_q == nq) { load_q = 0; ++load_h; }
+  };
+  if (tid == SOFT) {
     for (int i = 0; i < NS; ++i) {
       mbar_init(q_full + i, 1);
       mbar_init(q_empty + i, 1);
@@ -122,6 +137,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(l_empty + i, SOFT);
     }
     mbar_init(kv_full, 1);
+    mbar_init(kv_full + 1, 1);
     mbar_init(s_full, 1);
     mbar_init(s_read, SOFT);
     mbar_init(dp_full, 1);
@@ -130,10 +146,21 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_init(done, 1);
     *s_fail = 0;
     fence_mbar_init();
-    prefetch_tmap(&mq);
-    prefetch_tmap(&mk);
-    prefetch_tmap(&mv);
-    prefetch_tmap(&mg);
+    fence_proxy_async();
+    if (N > 0) {
+      load_h += it0 / nq;
+      load_q = it0 % nq;
+      mbar_expect_tx(kv_full, TB);
+      for (int s = 0; s < SL; ++s) tma_load_4d(sk + s * SLAB, &mk, kv_full, 64 * s, hk, j0, b);
+      load_q_tile(0);
+      mbar_expect_tx(kv_full + 1, TB);
+      for (int s = 0; s < SL; ++s) tma_load_4d(sv + s * SLAB, &mv, kv_full + 1, 64 * s, hk, j0, b);
+      load_g_tile(0);
+      for (loads = 1; loads < min(NS, N); ++loads) {
+        load_q_tile(loads);
+        load_g_tile(loads);
+      }
+    }
   }
   if (warp == 0) {
     tmem_alloc(s_tmem, 512);
@@ -149,28 +176,19 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8 && N > 0) {
       if (lane == 0) {  // ------------------------------------------------ loads
-        mbar_expect_tx(kv_full, 2 * TB);
-        for (int s = 0; s < SL; ++s) {
-          tma_load_4d(sk + s * SLAB, &mk, kv_full, 64 * s, hk, j0, b);
-          tma_load_4d(sv + s * SLAB, &mv, kv_full, 64 * s, hk, j0, b);
-        }
-        int qloads = 0, gloads = 0, h = hk * a.G + it0 / nq, qt = it0 % nq;
-        for (int n = 0; n < N; ++n) {
-          const int st = n % NS, par = (n / NS - 1) & 1, i0 = (first + qt) * TILE;
-          if (n >= NS && !wait(q_empty + st, par)) break;
-          mbar_expect_tx(q_full + st, TB);
-          for (int s = 0; s < SL; ++s) tma_load_4d(sq + st * TB + s * SLAB, &mq, q_full + st, 64 * s, h, i0, b);
-          ++qloads;
-          if (n >= NS && !wait(g_empty + st, par)) break;
-          mbar_expect_tx(g_full + st, TB);
-          for (int s = 0; s < SL; ++s) tma_load_4d(sg + st * TB + s * SLAB, &mg, g_full + st, 64 * s, h, i0, b);
-          ++gloads;
-          if (++qt == nq) { qt = 0; ++h; }
+        int n = loads;
+        for (; n < N; ++n) {
+          const int st = n % NS, par = (n / NS - 1) & 1;
+          if (!wait.lazy(q_empty + st, par)) break;
+          load_q_tile(n);
+          if (!wait.lazy(g_empty + st, par)) break;
+          load_g_tile(n);
         }
         if (*wait.fail) {  // copies in flight land before the CTA leaves
-          mbar_wait(kv_full, 0, kWait);
-          for (int m = max(0, qloads - NS); m < qloads; ++m) mbar_wait(q_full + m % NS, (m / NS) & 1, kWait >> 6);
-          for (int m = max(0, gloads - NS); m < gloads; ++m) mbar_wait(g_full + m % NS, (m / NS) & 1, kWait >> 6);
+          mbar_wait(kv_full, 0, kWait >> 6);
+          mbar_wait(kv_full + 1, 0, kWait >> 6);
+          for (int m = max(0, n - NS); m <= min(n, N - 1); ++m) mbar_wait(q_full + m % NS, (m / NS) & 1, kWait >> 6);
+          for (int m = max(0, n - NS); m < n; ++m) mbar_wait(g_full + m % NS, (m / NS) & 1, kWait >> 6);
         }
       }
     } else if (warp == 9 && N > 0) {  // ---------------------------------- products
@@ -195,7 +213,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           umma_commit(dp_full);
           return true;
         };
-        ok = ok && s_mma(0) && dp_mma(0);
+        ok = ok && s_mma(0) && wait(kv_full + 1, 0) && dp_mma(0);
         for (int n = 0; ok && n < N; ++n) {
           const int st = n % NS;
           if (n + 1 < N) {
@@ -352,7 +370,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (r == 0 && !part) {  // rows past T are not written
       for (int s = 0; s < SL; ++s) tma_store_4d(wg ? &mdk : &mdv, so + s * SLAB, 64 * s, hk, j0, b);
       bulk_commit();
-      bulk_wait_all();
+      bulk_wait_read();
     }
   }
   __syncwarp();
@@ -378,7 +396,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   unsigned char *sq = sm, *sg = sq + TB, *sk = sg + TB, *sv = sk + NK * TB;
   uint64_t *bars = reinterpret_cast<uint64_t *>(sv + NV * TB);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV;
-  uint64_t *s_full = v_empty + NV, *q_full = s_full + 2, *dp_full = q_full + 1, *dp_read = dp_full + 1;
+  uint64_t *s_full = v_empty + NV, *q_full = s_full + 2, *g_full = q_full + 1, *dp_full = g_full + 1, *dp_read = dp_full + 1;
   uint64_t *ds_full = dp_read + 1, *clean = ds_full + 1, *done = clean + 1;
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(done + 1);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
@@ -391,7 +409,21 @@ __global__ void __launch_bounds__(THREADS, 1)
   const SwaKeyTiles kt(i0, max(min(i0 + TILE, len), i0 + 1), a.W, a.ns, TILE);
   const int N = i0 < len ? kt.count : 0;
 
-  if (tid == 0) {
+  // the loading thread: the first stages are on their way before the CTA meets
+  int loads = 0;
+  auto load_k_tile = [&](int n) {
+    const int st = n % NK;
+    mbar_expect_tx(k_full + st, TB);
+    for (int s = 0; s < SL; ++s)
+      tma_load_4d(sk + st * TB + s * SLAB, &mk, k_full + st, 64 * s, hk, kt.at(n) * TILE, b);
+  };
+  auto load_v_tile = [&](int n) {
+    const int st = n % NV;
+    mbar_expect_tx(v_full + st, TB);
+    for (int s = 0; s < SL; ++s)
+      tma_load_4d(sv + st * TB + s * SLAB, &mv, v_full + st, 64 * s, hk, kt.at(n) * TILE, b);
+  };
+  if (tid == SOFT) {
     for (int i = 0; i < NK; ++i) {
       mbar_init(k_full + i, 1);
       mbar_init(k_empty + i, 1);
@@ -403,6 +435,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_init(s_full, 1);
     mbar_init(s_full + 1, 1);
     mbar_init(q_full, 1);
+    mbar_init(g_full, 1);
     mbar_init(dp_full, 1);
     mbar_init(dp_read, SOFT);
     mbar_init(ds_full, SOFT);
@@ -410,10 +443,19 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_init(done, 1);
     *s_fail = 0;
     fence_mbar_init();
-    prefetch_tmap(&mq);
-    prefetch_tmap(&mk);
-    prefetch_tmap(&mv);
-    prefetch_tmap(&mg);
+    fence_proxy_async();
+    if (N > 0) {
+      mbar_expect_tx(q_full, TB);
+      for (int s = 0; s < SL; ++s) tma_load_4d(sq + s * SLAB, &mq, q_full, 64 * s, h, i0, b);
+      load_k_tile(0);
+      mbar_expect_tx(g_full, TB);
+      for (int s = 0; s < SL; ++s) tma_load_4d(sg + s * SLAB, &mg, g_full, 64 * s, h, i0, b);
+      load_v_tile(0);
+      for (loads = 1; loads < min(NV, N); ++loads) {
+        load_k_tile(loads);
+        load_v_tile(loads);
+      }
+    }
   }
   if (warp == 0) {
     tmem_alloc(s_tmem, 512);
@@ -430,25 +472,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8 && N > 0) {
       if (lane == 0) {  // ------------------------------------------------ loads
-        mbar_expect_tx(q_full, 2 * TB);
-        for (int s = 0; s < SL; ++s) {
-          tma_load_4d(sq + s * SLAB, &mq, q_full, 64 * s, h, i0, b);
-          tma_load_4d(sg + s * SLAB, &mg, q_full, 64 * s, h, i0, b);
-        }
-        int kl = 0, vl = 0;
-        for (int n = 0; n < N; ++n) {
-          const int j0 = kt.at(n) * TILE, ks = n % NK, vs = n % NV;
-          if (n >= NK && !wait(k_empty + ks, (n / NK - 1) & 1)) break;
-          mbar_expect_tx(k_full + ks, TB);
-          for (int s = 0; s < SL; ++s) tma_load_4d(sk + ks * TB + s * SLAB, &mk, k_full + ks, 64 * s, hk, j0, b);
+        int kl = loads, vl = loads;
+        for (int n = loads; n < N; ++n) {
+          if (n >= NK && !wait.lazy(k_empty + n % NK, (n / NK - 1) & 1)) break;
+          load_k_tile(n);
           ++kl;
-          if (n >= NV && !wait(v_empty + vs, (n / NV - 1) & 1)) break;
-          mbar_expect_tx(v_full + vs, TB);
-          for (int s = 0; s < SL; ++s) tma_load_4d(sv + vs * TB + s * SLAB, &mv, v_full + vs, 64 * s, hk, j0, b);
+          if (n >= NV && !wait.lazy(v_empty + n % NV, (n / NV - 1) & 1)) break;
+          load_v_tile(n);
           ++vl;
         }
         if (*wait.fail) {  // copies in flight land before the CTA leaves
-          mbar_wait(q_full, 0, kWait);
+          mbar_wait(q_full, 0, kWait >> 6);
+          mbar_wait(g_full, 0, kWait >> 6);
           for (int m = max(0, kl - NK); m < kl; ++m) mbar_wait(k_full + m % NK, (m / NK) & 1, kWait >> 6);
           for (int m = max(0, vl - NV); m < vl; ++m) mbar_wait(v_full + m % NV, (m / NV) & 1, kWait >> 6);
         }
@@ -484,7 +519,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           umma_commit(v_empty + n % NV);
           return true;
         };
-        ok = ok && s_mma(0) && dp_mma(0);
+        ok = ok && s_mma(0) && wait(g_full, 0) && dp_mma(0);
         for (int n = 0; ok && n < N; ++n) {
           if (n + 1 < N) {
             if (!(ok = s_mma(n + 1))) break;
@@ -561,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (tid == 0) {  // rows past T are not written
       for (int s = 0; s < SL; ++s) tma_store_4d(&mdq, sq + s * SLAB, 64 * s, h, i0, b);
       bulk_commit();
-      bulk_wait_all();
+      bulk_wait_read();
     }
   }
   __syncwarp();

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (I.N == 0) continue;
         if (lane == 0) {
           auto load_q = [&](int x, int &n) {
-            if (n > 0 && !wait(q_empty + x, (n - 1) & 1)) return false;
+            if (n > 0 && !wait.lazy(q_empty + x, (n - 1) & 1)) return false;
             mbar_expect_tx(q_full + x, TB);
             for (int s = 0; s < SL; ++s)
               tma_load_4d(sq + x * TB + s * SLAB, &mq, q_full + x, 64 * s, I.h, I.i0 + x * TILE, I.b);
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           ok = load_q(0, qa) && (I.half[1].last < 0 || load_q(1, qb));
           for (int n = 0; ok && n < I.N; ++n) {
             const int st = kn % NS, par = (kn / NS - 1) & 1, t = I.kt.at(n);
-            if (kn >= NS && !(ok = wait(k_empty + st, par))) break;
+            if (kn >= NS && !(ok = wait.lazy(k_empty + st, par))) break;
             uint32_t f = I.ragged && n == I.N - 1 ? kRagged : 0u;
             for (int x = 0; x < 2; ++x)
               if (I.half[x].needs(t))
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int s = 0; s < SL; ++s)
               tma_load_4d(sk + st * TB + s * SLAB, &mk, k_full + st, 64 * s, I.hk, t * TILE, I.b);
             ++kn;
-            if (vn >= NS && !(ok = wait(v_empty + st, par))) break;
+            if (vn >= NS && !(ok = wait.lazy(v_empty + st, par))) break;
             mbar_expect_tx(v_full + st, TB);
             for (int s = 0; s < SL; ++s)
               tma_load_4d(sv + st * TB + s * SLAB, &mv, v_full + st, 64 * s, I.hk, t * TILE, I.b);

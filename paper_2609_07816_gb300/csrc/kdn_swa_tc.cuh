@@ -146,6 +146,19 @@ struct Waiter {
     atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
     return false;
   }
+  // by the loading thread and others that run ahead: they poll less often, since polls
+  // take issue slots from the warps that everything waits for
+  __device__ __forceinline__ bool lazy(uint64_t *bar, uint32_t parity) const {
+    if (mbar_try_wait(bar, parity)) return true;
+    for (uint32_t i = 0; i < kWait; ++i) {
+      __nanosleep(64);
+      if (mbar_try_wait(bar, parity)) return true;
+      if ((i & 15) == 15 && *fail) return false;
+    }
+    *fail = 1;
+    atomicExch(status, (unsigned)KDN_ERR_TIMEOUT);
+    return false;
+  }
   // by all lanes of a warp, which go on together
   __device__ __forceinline__ void warp(uint64_t *bar, uint32_t parity) const {
     (*this)(bar, parity);
