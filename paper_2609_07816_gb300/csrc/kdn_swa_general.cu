@@ -10,9 +10,13 @@
 // and columns tx + 16 j of a 64 x 64 product (i, j < 4), so that with rows of d + 4
 // floats both operands' 16-byte reads are free of bank conflicts, and two such
 // reads feed 16 multiply-adds.  The multiply-add rate bounds these kernels.
+#include <cooperative_groups.h>
+
 #include "kdn_swa.cuh"
 
 namespace kdn {
+
+namespace cg = cooperative_groups;
 
 SwaSplits swa_splits(const SwaArgs &a, int BM, int BN) {
   SwaSplits p{};
@@ -449,26 +453,29 @@ __global__ void __launch_bounds__(NT) k_swa_cache_fill(const SwaArgs a, uint4 *k
 }
 
 // One token over the cache: 8 lanes a key (d / 8 channels each), 32 keys at a time in
-// the CTA's 8 warps, a running softmax per group of lanes, joined through shared
-// memory.  One CTA owns one query head; the group's first head writes the new token
-// into its slot, and every head takes that slot's row from the inputs.
+// the CTA's 8 warps and two of them under way, a running softmax per group of lanes,
+// joined through shared memory.  A CTA, or a cluster of them that splits the slots,
+// serves one query head; the group's first head writes the new token into its slot, and
+// every head takes that slot's row from the inputs.
 template <typename DT, int D>
 __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, void *vc, const int *pos) {
-  constexpr int E = D / 8, GR = NT / 8;
-  __shared__ float s_m[GR], s_l[GR], s_o[GR][D];
+  constexpr int E = D / 8, GR = NT / 8, U = 2;
+  __shared__ float s_m[GR], s_l[GR], s_o[GR][D], s_part[D + 2];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = gridDim.x, rank = blockIdx.x;  // the cluster is the x axis of the grid
   const int tid = threadIdx.x, gr = tid / 8, ln = tid % 8;
-  const int h = blockIdx.x, b = blockIdx.y, hk = h / a.G;
+  const int h = blockIdx.y, b = blockIdx.z, hk = h / a.G;
   const int p = pos[b];
   const size_t out = ((size_t)b * a.H + h) * D;
-  if (p < 0) {
-    if (tid < D) st<DT>(a.o, out + tid, 0.f);
+  if (p < 0) {  // an idle sequence (the whole cluster leaves)
+    if (rank == 0 && tid < D) st<DT>(a.o, out + tid, 0.f);
     return;
   }
   const size_t S = (size_t)a.W + a.ns;
   const int slot = p < a.ns ? p : a.ns + (p - a.ns) % a.W;
   const int n = (int)min((long long)p + 1, (long long)S);
   const size_t base = ((size_t)b * a.Hk + hk) * S * D, in = ((size_t)b * a.Hk + hk) * D;
-  if (h % a.G == 0 && tid < D) {
+  if (h % a.G == 0 && rank == 0 && tid < D) {
     static_cast<DT *>(kc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.k)[in + tid];
     static_cast<DT *>(vc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.v)[in + tid];
   }
@@ -480,41 +487,66 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
     q[e] = ld<DT>(a.q, out + 32 * (e / 4) + 4 * ln + e % 4) * c2;
     o[e] = 0.f;
   }
-  for (int j0 = 0; j0 < n; j0 += GR) {  // the same trip count for every lane
-    const int j = j0 + gr;
-    const bool live = j < n;
-    const void *kp = j == slot ? a.k : kc, *vp = j == slot ? a.v : vc;
-    const size_t at = j == slot ? in : base + (size_t)(live ? j : 0) * D;
-    float s = 0.f, v[E];
+  for (int j0 = rank * U * GR; j0 < n; j0 += C * U * GR) {  // the same trip count for every lane
+    float s[U], v[U][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const size_t x = at + 32 * (e / 4) + 4 * ln + e % 4;
-      s = fmaf(q[e], live ? ld<DT>(kp, x) : 0.f, s);
-      v[e] = live ? ld<DT>(vp, x) : 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * GR + gr;
+      const bool live = j < n;
+      const void *kp = j == slot ? a.k : kc, *vp = j == slot ? a.v : vc;
+      const size_t at = j == slot ? in : base + (size_t)(live ? j : 0) * D;
+      s[u] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const size_t x = at + 32 * (e / 4) + 4 * ln + e % 4;
+        s[u] = fmaf(q[e], live ? ld<DT>(kp, x) : 0.f, s[u]);
+        v[u][e] = live ? ld<DT>(vp, x) : 0.f;
+      }
     }
 #pragma unroll
-    for (int w = 4; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-    if (!live) continue;
-    const float mn = fmaxf(m, s), f = exp2f(m - mn), pr = exp2f(s - mn);
-    m = mn;
-    l = fmaf(l, f, pr);
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], f, pr * v[e]);
+      for (int w = 4; w > 0; w >>= 1) s[u] += __shfl_xor_sync(0xffffffffu, s[u], w);
+      if (j0 + u * GR + gr >= n) continue;
+      const float mn = fmaxf(m, s[u]), f = exp2f(m - mn), pr = exp2f(s[u] - mn);
+      m = mn;
+      l = fmaf(l, f, pr);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], f, pr * v[u][e]);
+    }
   }
   if (ln == 0) { s_m[gr] = m; s_l[gr] = l; }
 #pragma unroll
   for (int e = 0; e < E; ++e) s_o[gr][32 * (e / 4) + 4 * ln + e % 4] = o[e];
   __syncthreads();
+  // a group (or a CTA) without keys has m = -inf and l = 0
+  auto factor = [](float x, float ref) { return x == -INFINITY ? 0.f : exp2f(x - ref); };
   if (tid < D) {
-    float mm = s_m[0], ls = 0.f, x = 0.f;  // group 0 always has the first key
-    for (int g = 1; g < GR; ++g) mm = fmaxf(mm, s_m[g]);
+    float mm = -INFINITY, ls = 0.f, x = 0.f;
+    for (int g = 0; g < GR; ++g) mm = fmaxf(mm, s_m[g]);
     for (int g = 0; g < GR; ++g) {
-      const float f = exp2f(s_m[g] - mm);
+      const float f = factor(s_m[g], mm);
       ls = fmaf(s_l[g], f, ls);
       x = fmaf(s_o[g][tid], f, x);
     }
+    if (C == 1) st<DT>(a.o, out + tid, x / ls);
+    s_part[tid] = x;
+    if (tid == 0) { s_part[D] = mm; s_part[D + 1] = ls; }
+  }
+  if (C == 1) return;
+  cluster.sync();
+  if (rank == 0 && tid < D) {
+    float mm = -INFINITY, ls = 0.f, x = 0.f;
+    for (int k = 0; k < C; ++k) mm = fmaxf(mm, cluster.map_shared_rank(s_part, k)[D]);
+    for (int k = 0; k < C; ++k) {
+      const float *r = cluster.map_shared_rank(s_part, k);
+      const float f = factor(r[D], mm);
+      ls = fmaf(r[D + 1], f, ls);
+      x = fmaf(r[tid], f, x);
+    }
     st<DT>(a.o, out + tid, x / ls);
   }
+  cluster.sync();  // no CTA leaves while another reads its part
 }
 
 kdn_status_t launched() { return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA; }
@@ -538,8 +570,20 @@ template <typename DT, int D> kdn_status_t bwd_t(const SwaArgs &a, const SwaSpli
 
 template <typename DT, int D>
 kdn_status_t dec_t(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
-  k_swa_decode<DT, D><<<dim3(a.H, a.B), NT, 0, s>>>(a, kc, vc, pos);
-  return launched();
+  // CTAs of a cluster: enough for two an SM, with four rounds of 64 keys each at least
+  int C = 1;
+  while (C < 8 && (long long)a.B * a.H * C < 2 * 152 && (long long)a.W + a.ns > C * 256LL) C *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(C, a.H, a.B);
+  cfg.blockDim = dim3(NT);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = C;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_swa_decode<DT, D>, a, kc, vc, pos) == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
 }
 
 }  // namespace
