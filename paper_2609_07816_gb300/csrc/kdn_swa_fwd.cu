@@ -86,10 +86,10 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS;
   uint64_t *s_full = v_empty + NS, *p_full = s_full + 2, *o_full = p_full + 2, *q_full = o_full + 2;
   uint64_t *q_empty = q_full + 2, *v_clean = q_empty + 2;
-  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(v_clean + 1 + 2 * kRing);
+  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(v_clean + NS + 2 * kRing);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
   volatile uint32_t *s_info = s_tmem + 2;  // [stage] what K's tile is to the products
-  const ItemRing ring{v_clean + 1, v_clean + 1 + kRing, reinterpret_cast<int *>(s_tmem + 2 + NS)};
+  const ItemRing ring{v_clean + NS, v_clean + NS + kRing, reinterpret_cast<int *>(s_tmem + 2 + NS)};
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(v_full + i, 1);
       mbar_init(k_empty + i, 1);
       mbar_init(v_empty + i, 1);
+      mbar_init(v_clean + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + i, 1);
@@ -106,7 +107,6 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(q_full + i, 1);
       mbar_init(q_empty + i, 1);
     }
-    mbar_init(v_clean, 1);
     for (int i = 0; i < kRing; ++i) {
       mbar_init(ring.full + i, 1);
       mbar_init(ring.empty + i, 8);  // the softmax warps
@@ -167,12 +167,12 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         __syncwarp();
         if (I.ragged) {  // the last tile's V past the length
-          const int m = __shfl_sync(0xffffffffu, vn, 0) - 1, st = m % NS;
+          const int m = __shfl_sync(0xffffffffu, vn, 0) - 1, st = max(m, 0) % NS;
           if (m >= 0) wait.warp(v_full + st, (m / NS) & 1);
           if (m >= 0) zero_rows(sv + st * TB, SL, I.len % TILE, lane);
           fence_proxy_async();
           __syncwarp();
-          if (lane == 0) mbar_arrive(v_clean);
+          if (lane == 0) mbar_arrive(v_clean + st);
         }
       }
       if (lane == 0) {
@@ -192,13 +192,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint64_t dq = desc_k(sq), dk = desc_k(sk), dv = desc_mn(sv);
         // of each accumulator: the tile whose P it is making (-1: none) and what that tile is
         // to it, its products P V and its items so far
-        int pending[2] = {-1, -1}, np[2] = {0, 0}, nq[2] = {0, 0}, clean = 0;
-        uint32_t what[2] = {0, 0};
+        int pending[2] = {-1, -1}, np[2] = {0, 0}, nq[2] = {0, 0};
+        uint32_t what[2] = {0, 0}, clean = 0;  // (clean: a stage's number of clearings, odd or even)
         auto pv = [&](int x) {  // O_x (+)= P_x V of its pending tile
           const int m = pending[x], st = m % NS;
           pending[x] = -1;
           if (!wait(v_full + st, (m / NS) & 1)) return false;
-          if ((what[x] & kRagged) && !wait(v_clean, clean++ & 1)) return false;
+          if (what[x] & kRagged) {
+            // of this stage: the loading warp may have cleared the tile of a later item too
+            if (!wait(v_clean + st, clean >> st & 1)) return false;
+            clean ^= 1u << st;
+          }
           if (!wait(p_full + x, np[x]++ & 1)) return false;
           tc_fence_after();
           const uint64_t d = dv + st * (TB >> 4);
@@ -213,7 +217,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         bool ok = true;
         for (int m = 0; ok; ++m) {
           const int st = m % NS;
-          if (!(ok = wait(k_full + st, (m / NS) & 1))) break;
+          if (!mbar_try_wait(k_full + st, (m / NS) & 1)) {
+            // The next tile may only come once the softmax warps have taken up later items,
+            // which they do after this one's last products.
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (ok && pending[x] >= 0 && (what[x] & kLast)) ok = pv(x);
+            if (!ok || !(ok = wait(k_full + st, (m / NS) & 1))) break;
+          }
           const uint32_t info = s_info[st];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {

@@ -1,6 +1,7 @@
 """Sliding-window attention with sinks on the GPU against its 64-bit definition:
 forward, gradients, cache and decode, at the sizes, windows, sinks, lengths and head
 groupings where tiles end raggedly and masks leave rows or tiles empty."""
+import ctypes
 import math
 
 import pytest
@@ -29,11 +30,18 @@ def make(seed, B, T, H, Hk, d, dtype):
     return rand(seed, (B, T, H, d), (B, T, Hk, d), (B, T, Hk, d), (B, T, H, d), dtype=dtype)
 
 
+def bwd_workspace(kdn, q, k, W, ns):
+    desc = kdn.make_swa_desc(*q.shape[:3], k.shape[2], q.shape[3], q.dtype, window=W, sinks=ns)
+    n = kdn.lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc))
+    return torch.full((n,), 255, dtype=torch.uint8, device="cuda")  # contents need no initialisation
+
+
 def run_and_check(kdn, q, k, v, dO, W, ns, lens=None, scale=None):
-    kw = dict(window=W, sinks=ns, lens=lens, scale=scale)
+    kw = dict(window=W, sinks=ns, lens=lens, scale=scale, workspace=bwd_workspace(kdn, q, k, W, ns))
     o, lse = kdn.kdn_swa_fwd(q, k, v, **kw)
+    assert kdn.kdn_get_device_status(kw["workspace"]) == kdn.KDN_OK  # no wait of the kernel ran out
     G = kdn.kdn_swa_bwd(q, k, v, o, lse, dO, **kw)
-    torch.cuda.synchronize()
+    assert kdn.kdn_get_device_status(kw["workspace"]) == kdn.KDN_OK
     clean = [x if lens is None else torch.where(
         (torch.arange(x.shape[1], device="cuda")[None] < lens[:, None])[:, :, None, None], x, 0) for x in (q, k, v, dO)]
     R = ref.attention(*clean[:3], W, ns, lens, scale, clean[3])
@@ -88,6 +96,30 @@ def test_padding_is_never_used(kdn, d, dtype):
         for x in (o, G["dq"], G["dk"], G["dv"]):
             assert not x[b, n:].any()
         assert (lse[b, :, n:] == -math.inf).all()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("T,step,empty", [(300, 7, 0), (130, 1, 0), (700, 97, 0), (300, 7, 40), (2000, 1, 44)])
+def test_many_short_padded_sequences(kdn, d, T, step, empty):
+    """Far more work items than CTAs, nearly all of them with a ragged last tile or with
+    nothing at all, one after another in the same CTA; passes that nothing waits between."""
+    B, H = 48, 8
+    lens = [(b * step + 1) % (T + 1) if b % 48 >= empty else 0 for b in range(B)]
+    q, k, v, dO = make(T, B, T, H, 2, d, BF)
+    for b, n in enumerate(lens):
+        for x in (q, k, v, dO):
+            x[b, n:] = math.nan
+    L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    kw = dict(window=60, sinks=3, lens=L)
+    runs = []
+    for _ in range(20):
+        o, lse = kdn.kdn_swa_fwd(q, k, v, workspace=ws, **kw)
+        runs.append((o, lse, *kdn.kdn_swa_bwd(q, k, v, o, lse, dO, **kw).values()))
+    assert kdn.kdn_get_device_status(ws) == kdn.KDN_OK
+    for r in runs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, runs[0]))
+    run_and_check(kdn, q, k, v, dO, 60, 3, L)
 
 
 def test_lengths_out_of_range_are_clamped(kdn):
@@ -171,10 +203,7 @@ def test_caller_buffers_streams_and_graphs(kdn):
     q, k, v, dO = make(40, 1, 260, 4, 2, 128, BF)
     o, lse = torch.empty_like(q), torch.empty(1, 4, 260, device="cuda")
     G = {n: torch.empty_like(x) for n, x in (("dq", q), ("dk", k), ("dv", v))}
-    desc = kdn.make_swa_desc(1, 260, 4, 2, 128, BF, window=64, sinks=2)
-    import ctypes
-    n = kdn.lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc))
-    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")  # contents need no initialisation
+    ws = bwd_workspace(kdn, q, k, 64, 2)
 
     def step(stream=None):
         kdn.kdn_swa_fwd(q, k, v, window=64, sinks=2, o=o, lse=lse, workspace=ws, stream=stream)
