@@ -5,7 +5,8 @@ The bounds are elementwise.  u = 2^-9 is the relative rounding of bfloat16, take
 twice (2^-8) for the stored result and for an operand rounded to bfloat16 (the
 weights P, and dS, where products run on the tensor cores); r32 covers float32:
 a score's sum of d products and the sums over n keys, as random rounding errors of
-2^-24 with a factor of 8 in hand.  delta = sum_d o dO is formed from the stored o."""
+2^-24 with a factor of 8 in hand.  delta = sum_d o dO is formed from the stored o, except
+for queries that see at most 64 keys, where it is formed from the keys."""
 import math
 
 import torch
@@ -58,7 +59,8 @@ def attention(q, k, v, W, ns, lens=None, scale=None, dO=None):
             dP, D = g @ V.T, (o * g).sum(1, keepdim=True)
             Da = (o * g).abs().sum(1, keepdim=True)
             dS = P * (dP - D)
-            E = up * dS.abs() + P * ((up + r32) * Da + r32 * (g.abs() @ V.abs().T))
+            far = (see.sum(1, keepdim=True) > 64).double()
+            E = up * dS.abs() + P * (far * up * Da + r32 * (Da + g.abs() @ V.abs().T))
             R["dq"][b, :n, h] = c * dS @ K
             R["edq"][b, :n, h] = c * (E + r32 * dS.abs()) @ K.abs()
             R["dk"][b, :n, hk] += c * dS.T @ Q
