@@ -355,9 +355,9 @@ kdn_status_t kdn_selftest_wait_timeout(void *workspace, void *stream);
  *            and gradients are 0, their lse is -inf, and what q, k, v and dO
  *            hold there (NaN included) is never used.
  *   Dtypes   q, k, v, dO, o, the caches and the gradients have desc->dtype.  Scores,
- *            softmax statistics and all sums are float32; with bfloat16 and
- *            d = 64 or 128 the weights (and in the backward dS) are rounded to
- *            bfloat16 as operands of the second products.
+ *            softmax statistics and all sums are float32; with bfloat16 the
+ *            weights (and in the backward dS) are rounded to bfloat16 as operands
+ *            of the second products.
  *   Sizes    d in {32, 64, 128}; H a multiple of Hk; T >= 0, at most 2^21; B, H <=
  *            65535; B*H*T <= 2^31 - 1; window >= 1, sinks >= 0, window + sinks <= 2^30.
  *   Order    Every sum has a fixed order: the same call gives the same bits.

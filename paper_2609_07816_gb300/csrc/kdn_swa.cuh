@@ -89,7 +89,7 @@ __device__ __forceinline__ int swa_split_rows(int t, int split, int per, int BN,
   return j0 < ns && q * BN - W >= j0 + BN - 1 ? min(BN, ns - j0) : BN;
 }
 
-// bfloat16 with d = 64 or 128 runs on the tensor cores
+// bfloat16 runs on the tensor cores, float32 on the general kernels
 bool swa_tc_supported(const SwaArgs &a);
 kdn_status_t launch_swa_fwd_tc(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_tc(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);

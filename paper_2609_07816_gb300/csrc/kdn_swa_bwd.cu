@@ -1,5 +1,6 @@
 // kdn_swa_bwd.cu -- gradients of the sliding-window attention with sinks on the tensor
-// cores (bfloat16, d = 64 or 128), from the forward's o and lse.
+// cores (bfloat16; d = 32 runs as 64 with the upper half of every row loaded as zeros),
+// from the forward's o and lse.
 //
 //   P = exp2(c2 S - nlse), dP = dO V^T, dS = P (dP - delta),
 //   dV = P^T dO, dK = c dS^T Q, dQ = c dS K
@@ -350,10 +351,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     unsigned char *so = wg ? sk : sv;
     const int rows = part ? swa_split_rows(t, split, per, TILE, a.W, a.ns, a.G, len) : TILE;
     if (part && 32 * (warp & 3) < rows) {
-      float *dst = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x) * (2 * TILE * D) + (wg ? 0 : TILE * D) +
-                   (size_t)r * D;
+      float *dst = a.part + (((size_t)b * a.Hk + hk) * sp.part_blocks + x) * (2 * TILE * a.d) +
+                   (wg ? 0 : TILE * a.d) + (size_t)r * a.d;
 #pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
+      for (int c = 0; c < a.d; c += 32) {
         float o[32];
         tmem_ld32(acc + c, o);  // rows > 0: the split has iterations
         tmem_ld_wait<32>(o);
@@ -607,10 +608,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 template <int D> kdn_status_t launch(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
   CUtensorMap mq, mk, mv, mg, mdq, mdk, mdv;
-  if (!token_map(&mq, a.q, a.B, a.T, a.H, D) || !token_map(&mk, a.k, a.B, a.T, a.Hk, D) ||
-      !token_map(&mv, a.v, a.B, a.T, a.Hk, D) || !token_map(&mg, a.dO, a.B, a.T, a.H, D) ||
-      !token_map(&mdq, a.dq, a.B, a.T, a.H, D) || !token_map(&mdk, a.dk, a.B, a.T, a.Hk, D) ||
-      !token_map(&mdv, a.dv, a.B, a.T, a.Hk, D))
+  if (!token_map(&mq, a.q, a.B, a.T, a.H, a.d) || !token_map(&mk, a.k, a.B, a.T, a.Hk, a.d) ||
+      !token_map(&mv, a.v, a.B, a.T, a.Hk, a.d) || !token_map(&mg, a.dO, a.B, a.T, a.H, a.d) ||
+      !token_map(&mdq, a.dq, a.B, a.T, a.H, a.d) || !token_map(&mdk, a.dk, a.B, a.T, a.Hk, a.d) ||
+      !token_map(&mdv, a.dv, a.B, a.T, a.Hk, a.d))
     return KDN_ERR_CUDA;
   if (cudaFuncSetAttribute(k_swa_dkv<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, KV_SMEM<D>) != cudaSuccess ||
       cudaFuncSetAttribute(k_swa_dq<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, DQ_SMEM<D>) != cudaSuccess)

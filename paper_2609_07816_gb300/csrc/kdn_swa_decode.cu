@@ -1,5 +1,5 @@
 // kdn_swa_decode.cu -- one token of every sequence over the bounded cache of the
-// sliding-window attention (bfloat16, d = 64 or 128).
+// sliding-window attention (bfloat16).
 //
 // The cache's filled slots are a prefix, and attention does not care for their order, so a
 // step is o = softmax(c q K^T) V over the first n slots: every byte of K and V is read once
@@ -67,6 +67,12 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ float factor(float m, float ref) { return m == -INFINITY ? 0.f : exp2f(m - ref); }
 
+// 16-byte column of a row of D bf16 in shared memory: rows that are read together lie in
+// different banks.
+template <int D> __device__ __forceinline__ int swz(int c, int r) {
+  return D >= 64 ? c ^ (r & 7) : c ^ (r >> 1 & 3);
+}
+
 template <int D>
 __global__ void __launch_bounds__(NT, 2)
     k_swa_decode_tc(const SwaArgs a, __nv_bfloat16 *kc, __nv_bfloat16 *vc, const int *pos, const int head_blocks) {
@@ -102,7 +108,7 @@ __global__ void __launch_bounds__(NT, 2)
         const int e = i * 32 + lane, r = e / VPR, c = e % VPR, j = ch * KN + r;
         const bool live = j < n;  // rows past n are zeros, whatever the cache holds
         const size_t at = base + (size_t)(live ? j : 0) * D + c * 8;
-        const uint32_t to = dst + r * ROW + ((c ^ (r & 7)) << 4);
+        const uint32_t to = dst + r * ROW + (swz<D>(c, r) << 4);
         copy16(to, j == slot ? kn + c * 8 : kc + at, live ? 16 : 0);
         copy16(to + CHUNK, j == slot ? vn + c * 8 : vc + at, live ? 16 : 0);
       }
@@ -149,7 +155,7 @@ __global__ void __launch_bounds__(NT, 2)
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
         uint32_t f[4];
-        ldsm4(f, sk + key * ROW + (((k * 2 + (mi & 1)) ^ (key & 7)) << 4));
+        ldsm4(f, sk + key * ROW + (swz<D>(k * 2 + (mi & 1), key) << 4));
         mma(s[t], q[k], f);
         mma(s[t + 1], q[k], f + 2);
       }
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(NT, 2)
 #pragma unroll
       for (int d = 0; d < D / 8; d += 2) {
         uint32_t g[4];
-        ldsm4t(g, sv + key * ROW + (((d + (mi >> 1)) ^ (key & 7)) << 4));
+        ldsm4t(g, sv + key * ROW + (swz<D>(d + (mi >> 1), key) << 4));
         mma(acc[d], w, g);
         mma(acc[d + 1], w, g + 2);
       }
@@ -306,7 +312,9 @@ kdn_status_t launch(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaSt
 }  // namespace
 
 kdn_status_t launch_swa_decode_tc(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
-  return a.d == 128 ? launch<128>(a, kc, vc, pos, s) : launch<64>(a, kc, vc, pos, s);
+  return a.d == 128  ? launch<128>(a, kc, vc, pos, s)
+         : a.d == 64 ? launch<64>(a, kc, vc, pos, s)
+                     : launch<32>(a, kc, vc, pos, s);
 }
 
 }  // namespace kdn

@@ -1,5 +1,5 @@
 // kdn_swa_fwd.cu -- sliding-window attention with sinks, forward, on the tensor cores
-// (bfloat16, d = 64 or 128).
+// (bfloat16; d = 32 runs as 64 with the upper half of every row loaded as zeros).
 //
 // A work item is 256 queries of one head, as two accumulators A and B of 128.  It goes once
 // over the keys they see, 128 at a time, with the running maximum and sum of a softmax:
@@ -20,7 +20,7 @@
 
 namespace kdn {
 
-bool swa_tc_supported(const SwaArgs &a) { return a.dtype == KDN_BF16 && a.d >= 64; }
+bool swa_tc_supported(const SwaArgs &a) { return a.dtype == KDN_BF16; }
 
 namespace {
 
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (a.lse && i < a.T)
         a.lse[((size_t)I.b * a.H + I.h) * a.T + i] = live ? (ref + log2f(l)) * kLn2 : -INFINITY;
       const float inv = live ? 1.f / l : 0.f;
-      __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.o) + (((size_t)I.b * a.T + i) * a.H + I.h) * D;
+      __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.o) + (((size_t)I.b * a.T + i) * a.H + I.h) * a.d;
       const bool any = hx.last >= 0;  // the accumulator has been written
       if (any) {
         wait.warp(o_full + x, done & 1);
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           tmem_ld32(to + c, o);
           tmem_ld_wait<32>(o);
         }
-        if (i < a.T) store_row32(dst + c, o, inv, live, wide);
+        if (i < a.T && (D == 128 || c < a.d)) store_row32(dst + c, o, inv, live, wide);
       }
     }
   }
@@ -359,8 +359,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 template <int D> kdn_status_t launch(const SwaArgs &a, cudaStream_t s) {
   CUtensorMap mq, mk, mv;
-  if (!token_map(&mq, a.q, a.B, a.T, a.H, D) || !token_map(&mk, a.k, a.B, a.T, a.Hk, D) ||
-      !token_map(&mv, a.v, a.B, a.T, a.Hk, D))
+  if (!token_map(&mq, a.q, a.B, a.T, a.H, a.d) || !token_map(&mk, a.k, a.B, a.T, a.Hk, a.d) ||
+      !token_map(&mv, a.v, a.B, a.T, a.Hk, a.d))
     return KDN_ERR_CUDA;
   if (cudaFuncSetAttribute(k_swa_fwd_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM<D>) != cudaSuccess)
     return KDN_ERR_CUDA;

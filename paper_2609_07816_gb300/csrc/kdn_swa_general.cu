@@ -1,6 +1,5 @@
 // kdn_swa_general.cu -- sliding-window attention with sinks on the CUDA cores:
-// float32 activations (any head dimension) and bfloat16 with d = 32, float32
-// arithmetic throughout; and the parts that every path shares (the backward's
+// float32 activations, float32 arithmetic throughout; and the parts that every path shares (the backward's
 // row sums, the join of split key tiles, the copy of a prompt into the cache).
 //
 //   s_ij = c q_i.k_j,  o_i = sum_j exp(s_ij - lse_i) v_j   over the keys that i sees
@@ -125,27 +124,17 @@ __device__ __forceinline__ void mm_nn(float (&acc)[4][D / 16], const float *P, c
   }
 }
 
-// Rows [r0, r0 + 64) of head h of a [B, T, heads, D] tensor into a float32 tile;
-// rows at and past `len` as zeros (whatever memory holds there).
-template <typename DT, int D>
+// Rows [r0, r0 + 64) of head h of a [B, T, heads, D] tensor as a tile; rows at and past
+// `len` as zeros (whatever memory holds there).
+template <int D>
 __device__ __forceinline__ void load_tile(float *dst, const void *src, int b, int h, int heads, int T, int r0,
                                           int len) {
   constexpr int V4 = D / 4;
   for (int e = threadIdx.x; e < BT * V4; e += NT) {
-    const int r = e / V4, c = (e % V4) * 4, t = r0 + r;
+    const int r = e / V4, c = e % V4, t = r0 + r;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (t < len) {
-      const size_t at = (((size_t)b * T + t) * heads + h) * D + c;
-      if constexpr (sizeof(DT) == 4) {
-        x = *reinterpret_cast<const float4 *>(static_cast<const float *>(src) + at);
-      } else {
-        const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(src) + at);
-        const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x));
-        const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y));
-        x = make_float4(lo.x, lo.y, hi.x, hi.y);
-      }
-    }
-    *reinterpret_cast<float4 *>(dst + r * LD<D> + c) = x;
+    if (t < len) x = static_cast<const float4 *>(src)[(((size_t)b * T + t) * heads + h) * V4 + c];
+    *reinterpret_cast<float4 *>(dst + r * LD<D> + 4 * c) = x;
   }
 }
 
@@ -163,7 +152,7 @@ __device__ __forceinline__ float row_max(float x) {
 
 template <int D> constexpr int FWD_SMEM = (2 * BT * LD<D> + (BT * LD<D> > BT * LP ? BT * LD<D> : BT * LP)) * 4;
 
-template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_fwd(const SwaArgs a) {
+template <int D> __global__ void __launch_bounds__(NT) k_swa_fwd(const SwaArgs a) {
   extern __shared__ __align__(16) float sm[];
   float *sq = sm, *sv = sq + BT * LD<D>, *sk = sv + BT * LD<D>, *sp = sk;  // P takes K's place
   constexpr int NC = D / 16;
@@ -174,14 +163,14 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_fwd(co
 #pragma unroll
   for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
   if (i0 < len) {
-    load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
+    load_tile<D>(sq, a.q, b, h, a.H, a.T, i0, len);
     const SwaKeyTiles kt(i0, i1, a.W, a.ns, BT);
     const float c2 = a.scale * kLog2e;
     for (int n = 0; n < kt.count; ++n) {
       const int j0 = kt.at(n) * BT;
       __syncthreads();
-      load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
-      load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+      load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+      load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
       __syncthreads();
       float s[4][4] = {};
       mm_nt<D>(s, sq, sk, ty, tx);
@@ -223,7 +212,7 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_fwd(co
     const float inv = live ? 1.f / ls : 0.f;
     const size_t at = (((size_t)b * a.T + qi) * a.H + h) * D;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) st<DT>(a.o, at + col_of<D>(tx, c), live ? o[i][c] * inv : 0.f);
+    for (int c = 0; c < NC; ++c) st<float>(a.o, at + col_of<D>(tx, c), live ? o[i][c] * inv : 0.f);
     if (a.lse && tx == 0)
       a.lse[((size_t)b * a.H + h) * a.T + qi] = live ? (m[i] + log2f(ls)) * kLn2 : -INFINITY;
   }
@@ -232,7 +221,7 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_fwd(co
 template <int D> constexpr int BWD_SMEM = (4 * BT * LD<D> + BT * LP + 2 * BT) * 4;
 
 // dQ of a query tile: one pass over the keys that it sees.
-template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq(const SwaArgs a) {
+template <int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq(const SwaArgs a) {
   extern __shared__ __align__(16) float sm[];
   float *sq = sm, *sg = sq + BT * LD<D>, *sk = sg + BT * LD<D>, *sv = sk + BT * LD<D>, *sd = sv + BT * LD<D>;
   constexpr int NC = D / 16;
@@ -241,8 +230,8 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq
   const int len = swa_len(a, b), i1 = min(i0 + BT, len);
   float acc[4][NC] = {};
   if (i0 < len) {
-    load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
-    load_tile<DT, D>(sg, a.dO, b, h, a.H, a.T, i0, len);
+    load_tile<D>(sq, a.q, b, h, a.H, a.T, i0, len);
+    load_tile<D>(sg, a.dO, b, h, a.H, a.T, i0, len);
     const size_t row0 = ((size_t)b * a.H + h) * a.T;
     float nl[4], de[4];
 #pragma unroll
@@ -256,8 +245,8 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq
     for (int n = 0; n < kt.count; ++n) {
       const int j0 = kt.at(n) * BT;
       __syncthreads();
-      load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
-      load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+      load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+      load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
       __syncthreads();
       float s[4][4] = {}, dp[4][4] = {};
       mm_nt<D>(s, sq, sk, ty, tx);
@@ -281,13 +270,13 @@ template <typename DT, int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq
     if (qi >= a.T) continue;
     const size_t at = (((size_t)b * a.T + qi) * a.H + h) * D;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) st<DT>(a.dq, at + col_of<D>(tx, c), acc[i][c] * a.scale);
+    for (int c = 0; c < NC; ++c) st<float>(a.dq, at + col_of<D>(tx, c), acc[i][c] * a.scale);
   }
 }
 
 // dK and dV of a split of a key tile: one pass over (query head of the group, query
 // tile) pairs.  Thread (ty, tx) holds P^T and dS^T of keys ty + 16 i, queries tx + 16 j.
-template <typename DT, int D>
+template <int D>
 __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSplits sp) {
   extern __shared__ __align__(16) float sm[];
   float *sk = sm, *sv = sk + BT * LD<D>, *sq = sv + BT * LD<D>, *sg = sq + BT * LD<D>, *st_ = sg + BT * LD<D>;
@@ -307,14 +296,14 @@ __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSp
     const int nq = last - first + 1;
     const int it1 = min((split + 1) * per, a.G * nq);
     const float c2 = a.scale * kLog2e;
-    load_tile<DT, D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
-    load_tile<DT, D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+    load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
+    load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
     for (int it = split * per; it < it1; ++it) {
       const int h = hk * a.G + it / nq, i0 = (first + it % nq) * BT;
       const size_t row0 = ((size_t)b * a.H + h) * a.T;
       __syncthreads();
-      load_tile<DT, D>(sq, a.q, b, h, a.H, a.T, i0, len);
-      load_tile<DT, D>(sg, a.dO, b, h, a.H, a.T, i0, len);
+      load_tile<D>(sq, a.q, b, h, a.H, a.T, i0, len);
+      load_tile<D>(sg, a.dO, b, h, a.H, a.T, i0, len);
       if (tid < BT) {
         snl[tid] = i0 + tid < len ? a.nlse[row0 + i0 + tid] : INFINITY;
         sde[tid] = i0 + tid < len ? a.delta[row0 + i0 + tid] : 0.f;
@@ -363,8 +352,8 @@ __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSp
     const size_t at = (((size_t)b * a.T + kj) * a.Hk + hk) * D;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      st<DT>(a.dk, at + col_of<D>(tx, c), dk[i][c] * a.scale);
-      st<DT>(a.dv, at + col_of<D>(tx, c), dv[i][c]);
+      st<float>(a.dk, at + col_of<D>(tx, c), dk[i][c] * a.scale);
+      st<float>(a.dv, at + col_of<D>(tx, c), dv[i][c]);
     }
   }
 }
@@ -543,7 +532,7 @@ __global__ void __launch_bounds__(NT) k_swa_cache_fill(const SwaArgs a, uint4 *k
 // joined through shared memory.  A CTA, or a cluster of them that splits the slots,
 // serves one query head; the group's first head writes the new token into its slot, and
 // every head takes that slot's row from the inputs.
-template <typename DT, int D>
+template <int D>
 __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, void *vc, const int *pos) {
   constexpr int E = D / 8, GR = NT / 8, U = 2;
   __shared__ float s_m[GR], s_l[GR], s_o[GR][D], s_part[D + 2];
@@ -554,7 +543,7 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
   const int p = pos[b];
   const size_t out = ((size_t)b * a.H + h) * D;
   if (p < 0) {  // an idle sequence (the whole cluster leaves)
-    if (rank == 0 && tid < D) st<DT>(a.o, out + tid, 0.f);
+    if (rank == 0 && tid < D) st<float>(a.o, out + tid, 0.f);
     return;
   }
   const size_t S = (size_t)a.W + a.ns;
@@ -562,15 +551,15 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
   const int n = (int)min((long long)p + 1, (long long)S);
   const size_t base = ((size_t)b * a.Hk + hk) * S * D, in = ((size_t)b * a.Hk + hk) * D;
   if (h % a.G == 0 && rank == 0 && tid < D) {
-    static_cast<DT *>(kc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.k)[in + tid];
-    static_cast<DT *>(vc)[base + (size_t)slot * D + tid] = static_cast<const DT *>(a.v)[in + tid];
+    static_cast<float *>(kc)[base + (size_t)slot * D + tid] = static_cast<const float *>(a.k)[in + tid];
+    static_cast<float *>(vc)[base + (size_t)slot * D + tid] = static_cast<const float *>(a.v)[in + tid];
   }
   // lane's channels: E / 4 runs of four, 32 apart
   const float c2 = a.scale * kLog2e;
   float q[E], o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    q[e] = ld<DT>(a.q, out + 32 * (e / 4) + 4 * ln + e % 4) * c2;
+    q[e] = ld<float>(a.q, out + 32 * (e / 4) + 4 * ln + e % 4) * c2;
     o[e] = 0.f;
   }
   for (int j0 = rank * U * GR; j0 < n; j0 += C * U * GR) {  // the same trip count for every lane
@@ -585,8 +574,8 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const size_t x = at + 32 * (e / 4) + 4 * ln + e % 4;
-        s[u] = fmaf(q[e], live ? ld<DT>(kp, x) : 0.f, s[u]);
-        v[u][e] = live ? ld<DT>(vp, x) : 0.f;
+        s[u] = fmaf(q[e], live ? ld<float>(kp, x) : 0.f, s[u]);
+        v[u][e] = live ? ld<float>(vp, x) : 0.f;
       }
     }
 #pragma unroll
@@ -615,7 +604,7 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
       ls = fmaf(s_l[g], f, ls);
       x = fmaf(s_o[g][tid], f, x);
     }
-    if (C == 1) st<DT>(a.o, out + tid, x / ls);
+    if (C == 1) st<float>(a.o, out + tid, x / ls);
     s_part[tid] = x;
     if (tid == 0) { s_part[D] = mm; s_part[D + 1] = ls; }
   }
@@ -630,7 +619,7 @@ __global__ void __launch_bounds__(NT) k_swa_decode(const SwaArgs a, void *kc, vo
       ls = fmaf(r[D + 1], f, ls);
       x = fmaf(r[tid], f, x);
     }
-    st<DT>(a.o, out + tid, x / ls);
+    st<float>(a.o, out + tid, x / ls);
   }
   cluster.sync();  // no CTA leaves while another reads its part
 }
@@ -641,20 +630,20 @@ template <typename K> bool smem_ok(K kernel, int bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
 }
 
-template <typename DT, int D> kdn_status_t fwd_t(const SwaArgs &a, cudaStream_t s) {
-  if (!smem_ok(k_swa_fwd<DT, D>, FWD_SMEM<D>)) return KDN_ERR_CUDA;
-  k_swa_fwd<DT, D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, FWD_SMEM<D>, s>>>(a);
+template <int D> kdn_status_t fwd_t(const SwaArgs &a, cudaStream_t s) {
+  if (!smem_ok(k_swa_fwd<D>, FWD_SMEM<D>)) return KDN_ERR_CUDA;
+  k_swa_fwd<D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, FWD_SMEM<D>, s>>>(a);
   return launched();
 }
 
-template <typename DT, int D> kdn_status_t bwd_t(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
-  if (!smem_ok(k_swa_bwd_dq<DT, D>, BWD_SMEM<D>) || !smem_ok(k_swa_bwd_dkv<DT, D>, BWD_SMEM<D>)) return KDN_ERR_CUDA;
-  k_swa_bwd_dkv<DT, D><<<dim3(sp.blocks, a.Hk, a.B), NT, BWD_SMEM<D>, s>>>(a, sp);
-  k_swa_bwd_dq<DT, D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, BWD_SMEM<D>, s>>>(a);
+template <int D> kdn_status_t bwd_t(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
+  if (!smem_ok(k_swa_bwd_dq<D>, BWD_SMEM<D>) || !smem_ok(k_swa_bwd_dkv<D>, BWD_SMEM<D>)) return KDN_ERR_CUDA;
+  k_swa_bwd_dkv<D><<<dim3(sp.blocks, a.Hk, a.B), NT, BWD_SMEM<D>, s>>>(a, sp);
+  k_swa_bwd_dq<D><<<dim3((a.T + BT - 1) / BT, a.H, a.B), NT, BWD_SMEM<D>, s>>>(a);
   return launched();
 }
 
-template <typename DT, int D>
+template <int D>
 kdn_status_t dec_t(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
   // CTAs of a cluster: enough for two an SM, with four rounds of 64 keys each at least
   int C = 1;
@@ -669,29 +658,23 @@ kdn_status_t dec_t(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStr
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_swa_decode<DT, D>, a, kc, vc, pos) == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, k_swa_decode<D>, a, kc, vc, pos) == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
 }
 
 }  // namespace
 
-#define KDN_SWA_BY_TYPE(fn, ...)                                                        \
-  do {                                                                                  \
-    if (a.dtype == KDN_BF16)                                                            \
-      return a.d == 128  ? fn<__nv_bfloat16, 128>(__VA_ARGS__)                          \
-             : a.d == 64 ? fn<__nv_bfloat16, 64>(__VA_ARGS__)                           \
-                         : fn<__nv_bfloat16, 32>(__VA_ARGS__);                          \
-    return a.d == 128 ? fn<float, 128>(__VA_ARGS__)                                     \
-           : a.d == 64 ? fn<float, 64>(__VA_ARGS__) : fn<float, 32>(__VA_ARGS__);       \
-  } while (0)
-
-kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s) { KDN_SWA_BY_TYPE(fwd_t, a, s); }
+kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s) {
+  return a.d == 128 ? fwd_t<128>(a, s) : a.d == 64 ? fwd_t<64>(a, s) : fwd_t<32>(a, s);
+}
 
 kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
-  KDN_SWA_BY_TYPE(bwd_t, a, sp, s);
+  return a.d == 128 ? bwd_t<128>(a, sp, s) : a.d == 64 ? bwd_t<64>(a, sp, s) : bwd_t<32>(a, sp, s);
 }
 
 kdn_status_t launch_swa_decode_general(const SwaArgs &a, void *kc, void *vc, const int *pos, cudaStream_t s) {
-  KDN_SWA_BY_TYPE(dec_t, a, kc, vc, pos, s);
+  return a.d == 128  ? dec_t<128>(a, kc, vc, pos, s)
+         : a.d == 64 ? dec_t<64>(a, kc, vc, pos, s)
+                     : dec_t<32>(a, kc, vc, pos, s);
 }
 
 template <int D> static kdn_status_t near_t(const SwaArgs &a, cudaStream_t s) {
