@@ -124,18 +124,34 @@ __device__ __forceinline__ void mm_nn(float (&acc)[4][D / 16], const float *P, c
   }
 }
 
-// Rows [r0, r0 + 64) of head h of a [B, T, heads, D] tensor as a tile; rows at and past
-// `len` as zeros (whatever memory holds there).
+// Rows [r0, r0 + 64) of head h of a [B, T, heads, D] tensor on their way into a tile, in
+// registers while the tile before them is worked on; rows at and past `len` are zeros
+// (whatever memory holds there).
+template <int D> struct Fetch {
+  static constexpr int V4 = D / 4, N = BT * V4 / NT;
+  float4 x[N];
+  __device__ __forceinline__ void load(const void *src, int b, int h, int heads, int T, int r0, int len) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = i * NT + threadIdx.x, t = r0 + e / V4;
+      x[i] = t < len ? static_cast<const float4 *>(src)[(((size_t)b * T + t) * heads + h) * V4 + e % V4]
+                     : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  __device__ __forceinline__ void store(float *dst) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = i * NT + threadIdx.x;
+      *reinterpret_cast<float4 *>(dst + (e / V4) * LD<D> + 4 * (e % V4)) = x[i];
+    }
+  }
+};
 template <int D>
 __device__ __forceinline__ void load_tile(float *dst, const void *src, int b, int h, int heads, int T, int r0,
                                           int len) {
-  constexpr int V4 = D / 4;
-  for (int e = threadIdx.x; e < BT * V4; e += NT) {
-    const int r = e / V4, c = e % V4, t = r0 + r;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (t < len) x = static_cast<const float4 *>(src)[(((size_t)b * T + t) * heads + h) * V4 + c];
-    *reinterpret_cast<float4 *>(dst + r * LD<D> + 4 * c) = x;
-  }
+  Fetch<D> f;
+  f.load(src, b, h, heads, T, r0, len);
+  f.store(dst);
 }
 
 // sum / max over the 16 threads of a row (tx = 0..15 of a half-warp)
@@ -169,6 +185,7 @@ template <int D> __global__ void __launch_bounds__(NT) k_swa_fwd(const SwaArgs a
     for (int n = 0; n < kt.count; ++n) {
       const int j0 = kt.at(n) * BT;
       __syncthreads();
+      // (the next tile on its way would take the second CTA of an SM: 2.0 for 1.75 ms at d = 128)
       load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
       load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
       __syncthreads();
@@ -242,12 +259,19 @@ template <int D> __global__ void __launch_bounds__(NT) k_swa_bwd_dq(const SwaArg
     }
     const SwaKeyTiles kt(i0, i1, a.W, a.ns, BT);
     const float c2 = a.scale * kLog2e;
+    Fetch<D> fk, fv;
+    fk.load(a.k, b, hk, a.Hk, a.T, kt.at(0) * BT, len);
+    fv.load(a.v, b, hk, a.Hk, a.T, kt.at(0) * BT, len);
     for (int n = 0; n < kt.count; ++n) {
       const int j0 = kt.at(n) * BT;
       __syncthreads();
-      load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
-      load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
+      fk.store(sk);
+      fv.store(sv);
       __syncthreads();
+      if (n + 1 < kt.count) {
+        fk.load(a.k, b, hk, a.Hk, a.T, kt.at(n + 1) * BT, len);
+        fv.load(a.v, b, hk, a.Hk, a.T, kt.at(n + 1) * BT, len);
+      }
       float s[4][4] = {}, dp[4][4] = {};
       mm_nt<D>(s, sq, sk, ty, tx);
       mm_nt<D>(dp, sg, sv, ty, tx);
@@ -298,17 +322,28 @@ __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSp
     const float c2 = a.scale * kLog2e;
     load_tile<D>(sk, a.k, b, hk, a.Hk, a.T, j0, len);
     load_tile<D>(sv, a.v, b, hk, a.Hk, a.T, j0, len);
-    for (int it = split * per; it < it1; ++it) {
+    Fetch<D> fq, fg;
+    float row_nl, row_de;
+    auto fetch = [&](int it) {
       const int h = hk * a.G + it / nq, i0 = (first + it % nq) * BT;
+      fq.load(a.q, b, h, a.H, a.T, i0, len);
+      fg.load(a.dO, b, h, a.H, a.T, i0, len);
       const size_t row0 = ((size_t)b * a.H + h) * a.T;
+      row_nl = tid < BT && i0 + tid < len ? a.nlse[row0 + i0 + tid] : INFINITY;
+      row_de = tid < BT && i0 + tid < len ? a.delta[row0 + i0 + tid] : 0.f;
+    };
+    if (split * per < it1) fetch(split * per);
+    for (int it = split * per; it < it1; ++it) {
+      const int i0 = (first + it % nq) * BT;
       __syncthreads();
-      load_tile<D>(sq, a.q, b, h, a.H, a.T, i0, len);
-      load_tile<D>(sg, a.dO, b, h, a.H, a.T, i0, len);
+      fq.store(sq);
+      fg.store(sg);
       if (tid < BT) {
-        snl[tid] = i0 + tid < len ? a.nlse[row0 + i0 + tid] : INFINITY;
-        sde[tid] = i0 + tid < len ? a.delta[row0 + i0 + tid] : 0.f;
+        snl[tid] = row_nl;
+        sde[tid] = row_de;
       }
       __syncthreads();
+      if (it + 1 < it1) fetch(it + 1);
       float s[4][4] = {}, dp[4][4] = {};
       mm_nt<D>(s, sk, sq, ty, tx);
       mm_nt<D>(dp, sv, sg, ty, tx);
