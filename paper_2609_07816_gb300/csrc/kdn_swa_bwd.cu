@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const Waiter wait{s_fail, a.status};
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8 && N > 0) {
       if (lane == 0) {  // ------------------------------------------------ loads
         int n = loads;
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   } else {  // ----------------------------------------------------------- pointwise
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int wg = warp >> 2, r = tid & 127, j = j0 + r, q0 = 64 * wg;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ts = TS + lanes + q0, tp = TP + lanes + q0;
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const bool ragged = len < a.T && N > 0 && kt.at(N - 1) * TILE + TILE > len;
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8 && N > 0) {
       if (lane == 0) {  // ------------------------------------------------ loads
         int kl = loads, vl = loads;
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   } else {  // ----------------------------------------------------------- pointwise
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int wg = warp >> 2, r = tid & 127, i = i0 + r, k0 = 64 * wg;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t tp = TP + lanes + k0;
