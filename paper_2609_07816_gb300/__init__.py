@@ -166,6 +166,9 @@ def _arg(t, name, dtype=None, numel=None, required=True):
         if required:
             raise ValueError(f"{name} is required")
         return
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()
+            and (dtype is None or t.dtype == dtype) and (numel is None or t.numel() == numel)):
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda:
@@ -612,29 +615,32 @@ def make_swa_desc(B, T, H, Hk, d, dtype, *, window, sinks=0, scale=None) -> kdn_
 def _check_swa(q, k, v, tokens=True):
     """q, k, v of one dtype: [B,T,H,d] and twice [B,T,Hk,d], without T for the decode step."""
     _arg(q, "q")
-    if q.dtype not in _DTYPES:
-        raise TypeError(f"q: dtype {q.dtype}, expected torch.float32 or torch.bfloat16")
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _arg(t, name, q.dtype)
-        if t.dim() != (4 if tokens else 3):
-            raise ValueError(f"{name}: {t.dim()} dimensions, expected {4 if tokens else 3}")
-    if k.shape[:-2] != q.shape[:-2] or k.shape[-1] != q.shape[-1]:
-        raise ValueError(f"k: shape {tuple(k.shape)} does not go with q's {tuple(q.shape)}")
-    if v.shape != k.shape:
-        raise ValueError(f"v: shape {tuple(v.shape)}, expected {tuple(k.shape)}")
+    dtype, dims = q.dtype, 4 if tokens else 3
+    if dtype not in _DTYPES:
+        raise TypeError(f"q: dtype {dtype}, expected torch.float32 or torch.bfloat16")
+    _arg(k, "k", dtype)
+    _arg(v, "v", dtype)
+    qs, ks, vs = q.shape, k.shape, v.shape
+    for shape, name in ((qs, "q"), (ks, "k"), (vs, "v")):
+        if len(shape) != dims:
+            raise ValueError(f"{name}: {len(shape)} dimensions, expected {dims}")
+    if ks[:-2] != qs[:-2] or ks[-1] != qs[-1]:
+        raise ValueError(f"k: shape {tuple(ks)} does not go with q's {tuple(qs)}")
+    if vs != ks:
+        raise ValueError(f"v: shape {tuple(vs)}, expected {tuple(ks)}")
 
 
 def _check_cache(kc, vc, k, window, sinks):
     shape = (k.shape[0], k.shape[-2], int(window) + int(sinks), k.shape[-1])
     for t, name in ((kc, "kc"), (vc, "vc")):
         _arg(t, name, k.dtype)
-        if tuple(t.shape) != shape:
+        if t.shape != shape:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
 
 
 def _swa_workspace(workspace, nbytes, device):
     if workspace is None:
-        workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
     _arg(workspace, "workspace", torch.uint8)
     return workspace
 
@@ -649,11 +655,13 @@ def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=
     desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if o is None:
         o = torch.empty_like(q)
-    if lse is None and want_lse:
+    else:
+        _arg(o, "o", q.dtype, q.numel())
+    if lse is not None:
+        _arg(lse, "lse", torch.float32, B * H * T)
+    elif want_lse:
         lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
     workspace = _swa_workspace(workspace, 256, q.device)
-    _arg(o, "o", q.dtype, q.numel())
-    _arg(lse, "lse", torch.float32, B * H * T, required=False)
     st = lib().kdn_swa_fwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o),
                            _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "kdn_swa_fwd")
@@ -673,8 +681,9 @@ def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, 
     desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if grads is None:
         grads = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
-    for n, x in (("dq", q), ("dk", k), ("dv", v)):
-        _arg(grads.get(n), n, q.dtype, x.numel())
+    else:
+        for n, x in (("dq", q), ("dk", k), ("dv", v)):
+            _arg(grads.get(n), n, q.dtype, x.numel())
     if workspace is None:
         workspace = _swa_workspace(None, lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc)), q.device)
     _arg(workspace, "workspace", torch.uint8)
@@ -708,7 +717,8 @@ def kdn_swa_decode_step(q, k, v, kc, vc, pos, *, window, sinks=0, scale=None, o=
     desc = make_swa_desc(B, 1, H, k.shape[1], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if o is None:
         o = torch.empty_like(q)
-    _arg(o, "o", q.dtype, q.numel())
+    else:
+        _arg(o, "o", q.dtype, q.numel())
     st = lib().kdn_swa_decode_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(kc), _ptr(vc),
                                    _ptr(pos), _ptr(o), _stream(stream))
     _check(st, "kdn_swa_decode_step")
@@ -734,23 +744,28 @@ def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=
     f8 = out_dtype == torch.float8_e4m3fn
     if not f8 and out_dtype != x.dtype:
         raise TypeError(f"out_dtype: {out_dtype}, expected {x.dtype} or torch.float8_e4m3fn")
-    D, lead = x.shape[-1], tuple(x.shape[:-1])
+    shape, n = x.shape, x.numel()
+    D = shape[-1]
     _arg(w, "w", x.dtype, D)
-    _arg(res, "res", x.dtype, x.numel(), required=False)
+    _arg(res, "res", x.dtype, n, required=False)
     desc = _norm_desc(x, KDN_F8E4M3 if f8 else _code(x.dtype), block, eps)
-    if y is None:
-        y = torch.empty(x.shape, dtype=out_dtype, device=x.device)
-    if h is None and res is not None:
-        h = torch.empty_like(x)
-    if rstd is None and want_rstd:
-        rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
     nb = -(-D // block) if block else 1
-    if f8 and scales is None:
-        scales = torch.empty(lead + (nb,), dtype=torch.float32, device=x.device)
-    _arg(y, "y", out_dtype, x.numel())
-    _arg(h, "h", x.dtype, x.numel(), required=False)
-    _arg(rstd, "rstd", torch.float32, desc.rows, required=False)
-    _arg(scales, "scales", torch.float32, desc.rows * nb, required=f8)
+    if y is None:
+        y = torch.empty_like(x, dtype=out_dtype)
+    else:
+        _arg(y, "y", out_dtype, n)
+    if h is not None:
+        _arg(h, "h", x.dtype, n)
+    elif res is not None:
+        h = torch.empty_like(x)
+    if rstd is not None:
+        _arg(rstd, "rstd", torch.float32, desc.rows)
+    elif want_rstd:
+        rstd = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
+    if scales is not None:
+        _arg(scales, "scales", torch.float32, desc.rows * nb)
+    elif f8:
+        scales = torch.empty(tuple(shape[:-1]) + (nb,), dtype=torch.float32, device=x.device)
     st = lib().kdn_add_rmsnorm_fwd(ctypes.byref(desc), _ptr(x), _ptr(res), _ptr(w), _ptr(y), _ptr(h),
                                    _ptr(rstd), _ptr(scales), _stream(stream))
     _check(st, "kdn_add_rmsnorm_fwd")
@@ -773,10 +788,12 @@ def kdn_add_rmsnorm_bwd(h, w, rstd, dy, dh=None, *, dx=None, dw=None, workspace=
     _arg(dh, "dh", h.dtype, h.numel(), required=False)
     if dx is None:
         dx = torch.empty_like(h)
+    else:
+        _arg(dx, "dx", h.dtype, h.numel())
     if dw is None:
         dw = torch.empty(D, dtype=torch.float32, device=h.device)
-    _arg(dx, "dx", h.dtype, h.numel())
-    _arg(dw, "dw", torch.float32, D)
+    else:
+        _arg(dw, "dw", torch.float32, D)
     if workspace is None:
         workspace = _swa_workspace(None, lib().kdn_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(desc)),
                                    h.device)
