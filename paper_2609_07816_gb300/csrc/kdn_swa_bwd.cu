@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t *bars = reinterpret_cast<uint64_t *>(sv + NV * TB);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV;
   uint64_t *s_full = v_empty + NV, *q_full = s_full + 2, *g_full = q_full + 1, *dp_full = g_full + 1, *dp_read = dp_full + 1;
-  uint64_t *ds_full = dp_read + 1, *clean = ds_full + 1, *done = clean + 1;
+  uint64_t *ds_full = dp_read + 1, *clean = ds_full + 2, *done = clean + 1;
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(done + 1);
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
 
@@ -440,6 +440,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_init(dp_full, 1);
     mbar_init(dp_read, SOFT);
     mbar_init(ds_full, SOFT);
+    mbar_init(ds_full + 1, SOFT);
     mbar_init(clean, 1);
     mbar_init(done, 1);
     *s_fail = 0;
@@ -528,7 +529,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc_fence_after();
             if (!(ok = dp_mma(n + 1))) break;
           }
-          if (!(ok = wait(ds_full, n & 1))) break;
+          if (!(ok = wait(ds_full + (n & 1), (n >> 1) & 1))) break;
           tc_fence_after();
           mma_t(TQ, tb + (n & 1) * 128, mk_ + off(n % NK), id_o, n > 0);
           umma_commit(n + 1 < N ? k_empty + n % NK : done);
@@ -586,7 +587,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       store32(ts, u);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(ds_full);
+      // Two barriers in turn: dP of tile n + 1 does not wait for dS of tile n, so threads of one
+      // half may come here with it before the other half's have with n.  (Nobody comes with
+      // n + 2 so early: its dP is issued behind the wait for dS of n.)
+      mbar_arrive(ds_full + (n & 1));
     }
     if (N > 0) wait.warp(done, 0);
     tc_fence_after();
