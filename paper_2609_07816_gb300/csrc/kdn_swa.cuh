@@ -39,6 +39,30 @@ __device__ __forceinline__ bool swa_sees(int i, int j, int W, int ns) {
   return j <= i && (j > i - W || j < ns);
 }
 
+// Two kernels of a call that need nothing of each other overlap: the first one's CTAs say
+// that the next may start once all of them have (its CTAs take the SMs that fall free), and
+// the next, launched with launch_beside, has one CTA wait for the first one's end, so that
+// what follows in the stream comes after both.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void end_after_previous() {
+  if (threadIdx.x == 0 && blockIdx.x + 1 == gridDim.x && blockIdx.y + 1 == gridDim.y && blockIdx.z + 1 == gridDim.z)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <typename... P, typename... A>
+kdn_status_t launch_beside(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, const A &...args) {
+  cudaLaunchAttribute beside{};
+  beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  beside.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = grid;
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  c.attrs = &beside;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
+}
+
 // Key tiles (of BN keys) that queries [i0, i1) see, i0 < i1: first the tiles of
 // the sinks that lie before the window, then the window's tiles up to the
 // diagonal.  Tile number n of the list is `at(n)`.

@@ -12,7 +12,8 @@
 //              them, for every query head of the group.  S^T and dP^T have keys as rows:
 //              P^T and dS^T go back to TMEM as bf16 A operands of dV and dK, both in the
 //              place of dP^T, so that the next S^T is formed while P and dS are.
-//   k_swa_dq   a CTA owns 128 queries and goes over the keys that they see.
+//   k_swa_dq   a CTA owns 128 queries and goes over the keys that they see.  Its CTAs start
+//              on the SMs that k_swa_dkv's last ones leave idle.
 // 256 threads do the pointwise part, each a row and 64 of its 128 columns (two threads
 // share a row), one warp loads, one thread issues the products.
 #include "kdn_swa_tc.cuh"
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  let_next_start();
   const int b = blockIdx.z, hk = blockIdx.y, x = blockIdx.x;
   const int nsx = sp.sink_tiles * sp.splits_sink;
   const int t = x < nsx ? x / sp.splits_sink : sp.sink_tiles + (x - nsx) / sp.splits;
@@ -608,6 +610,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tb, 512);
+  __syncwarp();
+  end_after_previous();
 }
 
 template <int D> kdn_status_t launch(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s) {
@@ -621,8 +625,9 @@ template <int D> kdn_status_t launch(const SwaArgs &a, const SwaSplits &sp, cuda
       cudaFuncSetAttribute(k_swa_dq<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, DQ_SMEM<D>) != cudaSuccess)
     return KDN_ERR_CUDA;
   k_swa_dkv<D><<<dim3(sp.blocks, a.Hk, a.B), THREADS, KV_SMEM<D>, s>>>(mq, mk, mv, mg, mdk, mdv, a, sp);
-  k_swa_dq<D><<<dim3((a.T + TILE - 1) / TILE, a.H, a.B), THREADS, DQ_SMEM<D>, s>>>(mq, mk, mv, mg, mdq, a);
-  return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
+  if (cudaGetLastError() != cudaSuccess) return KDN_ERR_CUDA;
+  return launch_beside(k_swa_dq<D>, dim3((a.T + TILE - 1) / TILE, a.H, a.B), THREADS, DQ_SMEM<D>, s, mq, mk, mv, mg,
+                       mdq, a);
 }
 
 }  // namespace
