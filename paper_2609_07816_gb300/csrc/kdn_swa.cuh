@@ -44,9 +44,10 @@ __device__ __forceinline__ bool swa_sees(int i, int j, int W, int ns) {
 // the next, launched with launch_beside, has one CTA wait for the first one's end, so that
 // what follows in the stream comes after both.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void end_after_previous() {
   if (threadIdx.x == 0 && blockIdx.x + 1 == gridDim.x && blockIdx.y + 1 == gridDim.y && blockIdx.z + 1 == gridDim.z)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_previous();
 }
 template <typename... P, typename... A>
 kdn_status_t launch_beside(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, const A &...args) {

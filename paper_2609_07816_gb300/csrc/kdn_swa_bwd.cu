@@ -101,7 +101,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   int *s_fail = reinterpret_cast<int *>(s_tmem + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  let_next_start();
   const int b = blockIdx.z, hk = blockIdx.y, x = blockIdx.x;
   const int nsx = sp.sink_tiles * sp.splits_sink;
   const int t = x < nsx ? x / sp.splits_sink : sp.sink_tiles + (x - nsx) / sp.splits;
@@ -236,6 +235,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
       }
     } else if (warp == 10) {  // --------------------------------------- row sums
+      // everything else may start before the row sums are there; k_swa_dq, which reads them
+      // too, after this
+      wait_for_previous();
+      let_next_start();
       int g = it0 / max(nq, 1), qt = it0 % max(nq, 1);
       for (int n = 0; n < N; ++n) {
         const int st = n % NR, h = hk * a.G + g, i0 = (first + qt) * TILE;
@@ -545,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t tp = TP + lanes + k0;
     const float c2 = a.scale * kLog2e;
     const size_t row = ((size_t)b * a.H + h) * a.T + i;
-    const float nl = i < len ? -a.nlse[row] : -INFINITY, de = i < len ? -a.delta[row] : 0.f;
+    const float nl = i < len ? -__ldcg(a.nlse + row) : -INFINITY, de = i < len ? -__ldcg(a.delta + row) : 0.f;
     const float2 cc = make_float2(c2, c2), nn = make_float2(nl, nl), dd = make_float2(de, de);
     for (int n = 0; n < N; ++n) {
       const int j0 = kt.at(n) * TILE;
@@ -624,8 +627,9 @@ template <int D> kdn_status_t launch(const SwaArgs &a, const SwaSplits &sp, cuda
   if (cudaFuncSetAttribute(k_swa_dkv<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, KV_SMEM<D>) != cudaSuccess ||
       cudaFuncSetAttribute(k_swa_dq<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, DQ_SMEM<D>) != cudaSuccess)
     return KDN_ERR_CUDA;
-  k_swa_dkv<D><<<dim3(sp.blocks, a.Hk, a.B), THREADS, KV_SMEM<D>, s>>>(mq, mk, mv, mg, mdk, mdv, a, sp);
-  if (cudaGetLastError() != cudaSuccess) return KDN_ERR_CUDA;
+  const kdn_status_t st = launch_beside(k_swa_dkv<D>, dim3(sp.blocks, a.Hk, a.B), THREADS, KV_SMEM<D>, s, mq, mk, mv,
+                                        mg, mdk, mdv, a, sp);
+  if (st != KDN_OK) return st;
   return launch_beside(k_swa_dq<D>, dim3((a.T + TILE - 1) / TILE, a.H, a.B), THREADS, DQ_SMEM<D>, s, mq, mk, mv, mg,
                        mdq, a);
 }

@@ -393,11 +393,18 @@ __global__ void __launch_bounds__(NT) k_swa_bwd_dkv(const SwaArgs a, const SwaSp
   }
 }
 
+// A query that sees at most kNear keys; bfloat16 forms its delta from them.
+constexpr int kNear = 64;
+__device__ __forceinline__ bool near(int i, const SwaArgs &a) {
+  return min(i + 1, a.W) + min(max(i + 1 - a.W, 0), a.ns) <= kNear;
+}
+
 // delta_i = sum_d o_id dO_id, and lse in log2 units.  Rows past the length get +inf, so
 // that their weights are exp2(-inf) = 0.  LPR lanes share a row, 16 bytes each; a CTA
 // takes 4 NT / LPR tokens of a head, so that its row sums leave in one run of memory.
 // Reads 2 d elements a row: bandwidth.
 template <typename DT, int LPR> __global__ void __launch_bounds__(NT) k_swa_prep(const SwaArgs a) {
+  let_next_start();
   constexpr int V = 16 / (int)sizeof(DT), RPP = NT / LPR, PASSES = 4;
   const int b = blockIdx.z, h = blockIdx.y, len = swa_len(a, b);
   const int ln = threadIdx.x % LPR, t0 = blockIdx.x * RPP * PASSES + threadIdx.x / LPR;
@@ -421,12 +428,13 @@ template <typename DT, int LPR> __global__ void __launch_bounds__(NT) k_swa_prep
     if (ln == 0 && t < a.T) {
       const size_t out = ((size_t)b * a.H + h) * a.T + t;
       a.nlse[out] = t < len ? a.lse[out] * kLog2e : INFINITY;
-      a.delta[out] = s;
+      if (sizeof(DT) == 4 || t >= len || !near(t, a)) a.delta[out] = s;
     }
   }
+  if (sizeof(DT) == 2) end_after_previous();  // k_swa_near
 }
 
-// delta of queries that see at most kNear keys, from the keys: sum_j P_ij dP_ij.  The
+// delta of queries that see at most kNear keys (k_swa_prep, beside it, leaves them out), from the keys: sum_j P_ij dP_ij.  The
 // stored o is rounded to bfloat16, and where it averages few values that rounding weighs
 // as much as the gradients' own (two tokens of d = 64: dk 5.1e-3 off, against 1.7e-3).
 // Far rows keep sum_d o dO: there it is 3 % of the error.  Only the first 64 queries of a
@@ -436,8 +444,6 @@ template <typename DT, int LPR> __global__ void __launch_bounds__(NT) k_swa_prep
 // m16n8k16 products of rows as they lie in memory (exact products, float32 sums).  Lane
 // c = lane % 4 of a row holds channels 32 m + 8 c .. + 7: the products sum over the
 // channels in that order, the same for both operands, so that every load is 16 bytes.
-constexpr int kNear = 64;
-
 __device__ __forceinline__ void mma_near(float *c, const uint32_t *a, const uint32_t *b) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
@@ -448,11 +454,11 @@ __device__ __forceinline__ void mma_near(float *c, const uint32_t *a, const uint
 
 template <int D> __global__ void __launch_bounds__(128) k_swa_near(const SwaArgs a) {
   constexpr int M = D / 32;  // 16-byte loads of a lane for a row
+  let_next_start();
   __shared__ float part[4][16];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, b = blockIdx.z, h = blockIdx.y, hk = h / a.G;
   const int i0 = blockIdx.x * 16, len = swa_len(a, b);
-  auto sees = [&](int i) { return min(i + 1, a.W) + min(max(i + 1 - a.W, 0), a.ns); };
-  if (i0 >= len || sees(i0) > kNear) return;
+  if (i0 >= len || !near(i0, a)) return;
   const int r = lane >> 2, c = lane & 3, last = min(i0 + 15, len - 1);
   uint4 q[M][2], g[M][2];
 #pragma unroll
@@ -465,7 +471,7 @@ template <int D> __global__ void __launch_bounds__(128) k_swa_near(const SwaArgs
     }
   }
   const size_t row0 = ((size_t)b * a.H + h) * a.T;
-  const float nl[2] = {a.nlse[row0 + min(i0 + r, last)], a.nlse[row0 + min(i0 + r + 8, last)]};
+  const float nl[2] = {a.lse[row0 + min(i0 + r, last)] * kLog2e, a.lse[row0 + min(i0 + r + 8, last)] * kLog2e};
   const float c2 = a.scale * kLog2e;
   const SwaKeyTiles kt(i0, last + 1, a.W, a.ns, 8);
   float de[2] = {0.f, 0.f};
@@ -508,7 +514,7 @@ template <int D> __global__ void __launch_bounds__(128) k_swa_near(const SwaArgs
   }
   __syncthreads();
   const int i = i0 + threadIdx.x;
-  if (threadIdx.x < 16 && i <= last && sees(i) <= kNear)
+  if (threadIdx.x < 16 && i <= last && near(i, a))
     a.delta[row0 + i] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
 }
 
@@ -722,17 +728,17 @@ kdn_status_t launch_swa_prep(const SwaArgs &a, cudaStream_t s) {
   const int lpr = a.d * (a.dtype == KDN_BF16 ? 2 : 4) / 16, rows = 4 * NT / lpr;
   const dim3 grid((a.T + rows - 1) / rows, a.H, a.B);
   if (a.dtype == KDN_BF16) {
-    if (lpr == 16) k_swa_prep<__nv_bfloat16, 16><<<grid, NT, 0, s>>>(a);
-    else if (lpr == 8) k_swa_prep<__nv_bfloat16, 8><<<grid, NT, 0, s>>>(a);
-    else k_swa_prep<__nv_bfloat16, 4><<<grid, NT, 0, s>>>(a);
-  } else {
-    if (lpr == 32) k_swa_prep<float, 32><<<grid, NT, 0, s>>>(a);
-    else if (lpr == 16) k_swa_prep<float, 16><<<grid, NT, 0, s>>>(a);
-    else k_swa_prep<float, 8><<<grid, NT, 0, s>>>(a);
+    const kdn_status_t st = a.d == 128 ? near_t<128>(a, s) : a.d == 64 ? near_t<64>(a, s) : near_t<32>(a, s);
+    if (st != KDN_OK) return st;
+    return launch_beside(lpr == 16  ? k_swa_prep<__nv_bfloat16, 16>
+                         : lpr == 8 ? k_swa_prep<__nv_bfloat16, 8>
+                                    : k_swa_prep<__nv_bfloat16, 4>,
+                         grid, NT, 0, s, a);
   }
-  if (launched() != KDN_OK) return KDN_ERR_CUDA;
-  if (a.dtype != KDN_BF16) return KDN_OK;
-  return a.d == 128 ? near_t<128>(a, s) : a.d == 64 ? near_t<64>(a, s) : near_t<32>(a, s);
+  if (lpr == 32) k_swa_prep<float, 32><<<grid, NT, 0, s>>>(a);
+  else if (lpr == 16) k_swa_prep<float, 16><<<grid, NT, 0, s>>>(a);
+  else k_swa_prep<float, 8><<<grid, NT, 0, s>>>(a);
+  return launched();
 }
 
 kdn_status_t launch_swa_join(const SwaArgs &a, const SwaSplits &sp, int BN, cudaStream_t s) {
