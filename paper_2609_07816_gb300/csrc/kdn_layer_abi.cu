@@ -117,9 +117,9 @@ kdn_status_t kdn_swa_fwd(const kdn_swa_desc_t *desc, const void *q, const void *
   a.q = q; a.k = k; a.v = v; a.lens = lens; a.o = o; a.lse = lse;
   a.status = static_cast<unsigned *>(workspace);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // the status word, and the counter of work items behind it
-  if (cudaMemsetAsync(a.status, 0, 2 * sizeof(unsigned), s) != cudaSuccess) return KDN_ERR_CUDA;
-  return swa_tc_supported(a) ? launch_swa_fwd_tc(a, s) : launch_swa_fwd_general(a, s);
+  if (swa_tc_supported(a)) return launch_swa_fwd_tc(a, s);
+  if (cudaMemsetAsync(a.status, 0, sizeof(unsigned), s) != cudaSuccess) return KDN_ERR_CUDA;
+  return launch_swa_fwd_general(a, s);
 }
 
 kdn_status_t kdn_swa_bwd(const kdn_swa_desc_t *desc, const void *q, const void *k, const void *v, const int *lens,

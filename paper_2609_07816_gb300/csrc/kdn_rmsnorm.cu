@@ -11,6 +11,7 @@
 // HBM traffic bounds both directions.
 #include <cuda_fp8.h>
 
+#include "kdn_beside.cuh"
 #include "kdn_internal.cuh"
 #include "kdn_rmsnorm.cuh"
 
@@ -167,12 +168,13 @@ __global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm(const NormArgs a) {
 // WARP: a row a warp, four of them a CTA (up to 512 columns, EPT 8 or 16).  Otherwise a
 // CTA a row, with as many threads as it has groups of EPT = 8 elements (16 beyond
 // 8192, without the early loads, for which 64 registers do not suffice): no registers
-// idle, and 1024 threads an SM whatever the width.  5.4 TB/s at 32768 x 2048 (99 us, the
+// idle, and 1024 threads an SM whatever the width.  5.6 TB/s at 32768 x 2048 (96 us, the
 // join of dw included); 128 threads of 16 elements each, without early loads: 3.4 TB/s.
 template <typename DT, int EPT, bool WARP>
 __global__ void __launch_bounds__(WARP ? 128 : 1024, WARP ? 4 : 1) k_add_rmsnorm_bwd(const NormArgs a) {
   constexpr int V = EV<DT>, NV = EPT / V;
   constexpr bool AHEAD = WARP || EPT == 8;
+  let_next_start();
   __shared__ float red[2][32];
   __shared__ __align__(16) float s_dw[WARP ? 4 * 32 * EPT : 1];
   const int TPR = WARP ? 32 : blockDim.x, RPC = WARP ? 4 : 1;
@@ -268,6 +270,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024, WARP ? 4 : 1) k_add_rmsnorm
 __global__ void __launch_bounds__(1024) k_rmsnorm_dw(const float *part, int n, int D, float *dw) {
   __shared__ float s[32][33];
   const int cx = threadIdx.x % 32, ry = threadIdx.x / 32, c = blockIdx.x * 32 + cx;
+  wait_for_previous();
   float x = 0.f;
   if (c < D)
     for (int r = ry; r < n; r += 32) x += part[(size_t)r * D + c];
@@ -321,10 +324,9 @@ template <typename DT> kdn_status_t bwd_t(const NormArgs &a, cudaStream_t s) {
     else if (a.D <= 512) k_add_rmsnorm_bwd<DT, 16, true><<<n, nt, 0, s>>>(a);
     else if (a.D <= 8192) k_add_rmsnorm_bwd<DT, 8, false><<<n, nt, 0, s>>>(a);
     else k_add_rmsnorm_bwd<DT, 16, false><<<n, nt, 0, s>>>(a);
-    if (launched() != KDN_OK) return KDN_ERR_CUDA;
   }
-  k_rmsnorm_dw<<<(a.D + 31) / 32, 1024, 0, s>>>(a.part, n, a.D, a.dw);
-  return launched();
+  if (launched() != KDN_OK) return KDN_ERR_CUDA;
+  return launch_beside(k_rmsnorm_dw, dim3((a.D + 31) / 32), 1024, 0, s, (const float *)a.part, n, a.D, a.dw);
 }
 
 }  // namespace

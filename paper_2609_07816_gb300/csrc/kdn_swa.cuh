@@ -5,6 +5,7 @@
 // (j > i - W or j < s): the last W tokens up to itself, and the first s.
 #pragma once
 
+#include "kdn_beside.cuh"
 #include "kdn_internal.cuh"
 
 namespace kdn {
@@ -37,31 +38,6 @@ __device__ __forceinline__ int swa_len(const SwaArgs &a, int b) {
 
 __device__ __forceinline__ bool swa_sees(int i, int j, int W, int ns) {
   return j <= i && (j > i - W || j < ns);
-}
-
-// Two kernels of a call that need nothing of each other overlap: the first one's CTAs say
-// that the next may start once all of them have (its CTAs take the SMs that fall free), and
-// the next, launched with launch_beside, has one CTA wait for the first one's end, so that
-// what follows in the stream comes after both.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void end_after_previous() {
-  if (threadIdx.x == 0 && blockIdx.x + 1 == gridDim.x && blockIdx.y + 1 == gridDim.y && blockIdx.z + 1 == gridDim.z)
-    wait_for_previous();
-}
-template <typename... P, typename... A>
-kdn_status_t launch_beside(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, const A &...args) {
-  cudaLaunchAttribute beside{};
-  beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  beside.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t c{};
-  c.gridDim = grid;
-  c.blockDim = dim3(threads);
-  c.dynamicSmemBytes = smem;
-  c.stream = s;
-  c.attrs = &beside;
-  c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, kernel, args...) == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
 }
 
 // Key tiles (of BN keys) that queries [i0, i1) see, i0 < i1: first the tiles of
@@ -122,7 +98,7 @@ kdn_status_t launch_swa_decode_tc(const SwaArgs &a, void *kc, void *vc, const in
 constexpr int kSwaTcTile = 128;  // query and key tile of the tensor-core kernels
 kdn_status_t launch_swa_fwd_general(const SwaArgs &a, cudaStream_t s);
 kdn_status_t launch_swa_bwd_general(const SwaArgs &a, const SwaSplits &sp, cudaStream_t s);
-// delta, nlse and a cleared status word: the first launch of every backward
+// delta, nlse and a cleared status word: the first launches of every backward
 kdn_status_t launch_swa_prep(const SwaArgs &a, cudaStream_t s);
 // adds the partial sums of split key tiles into dk, dv
 kdn_status_t launch_swa_join(const SwaArgs &a, const SwaSplits &sp, int BN, cudaStream_t s);

@@ -73,6 +73,12 @@ struct Item {
 constexpr uint32_t kNeeds = 1, kFirst = 2, kLast = 4, kFrees = 8;  // (kFrees: set by the issuing thread)
 constexpr uint32_t kRagged = 1u << 16, kEnd = 1u << 17;
 
+// The status word and the counter of work items.
+__global__ void k_swa_clear(unsigned *status) {
+  let_next_start();
+  if (threadIdx.x < 2) status[threadIdx.x] = 0;
+}
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
     k_swa_fwd_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
@@ -132,6 +138,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp == 8) {  // --------------------------------------------------- loads
       int kn = 0, vn = 0, qa = 0, qb = 0;  // loads issued (K and V: tiles, Q: items)
       bool ok = true;
+      wait_for_previous();  // the counter is clear
       ItemSource work(ring, wait, a.status + 1, S.items);
       for (int item; (item = work.next()) >= 0;) {
         const Item I(a, S, item);
@@ -366,8 +373,9 @@ template <int D> kdn_status_t launch(const SwaArgs &a, cudaStream_t s) {
     return KDN_ERR_CUDA;
   const int blocks = (a.T + 2 * TILE - 1) / (2 * TILE);
   const Shape S{blocks * a.H * a.B, blocks, FastDiv(blocks), FastDiv(a.H), FastDiv(a.G)};
-  k_swa_fwd_tc<D><<<S.items < kCtas ? S.items : kCtas, THREADS, SMEM<D>, s>>>(mq, mk, mv, a, S);
-  return cudaGetLastError() == cudaSuccess ? KDN_OK : KDN_ERR_CUDA;
+  k_swa_clear<<<1, 32, 0, s>>>(a.status);
+  if (cudaGetLastError() != cudaSuccess) return KDN_ERR_CUDA;
+  return launch_beside(k_swa_fwd_tc<D>, dim3(S.items < kCtas ? S.items : kCtas), THREADS, SMEM<D>, s, mq, mk, mv, a, S);
 }
 
 }  // namespace
