@@ -415,7 +415,8 @@ kdn_status_t kdn_swa_decode_step(const kdn_swa_desc_t *desc, const void *q, cons
      out_dtype = KDN_F8E4M3: y holds e4m3 bytes q with y ~ q * scale,
        scale = max |y| / 448 over the row (block 0) or over each 128 columns
        (block 128; the last block may be shorter), 1 where that maximum is 0 or
-       not finite.  scales [rows] or [rows, ceil(D / 128)] float32.
+       not finite; below float32's normal range it is rounded up and so never 0.
+       scales [rows] or [rows, ceil(D / 128)] float32.
    Sizes: D a multiple of 8, at most 16384; rows at most 2^31 - 1. */
 typedef struct {
   long long rows;

@@ -2,7 +2,7 @@
 // the activations' type or in 8 bits with scales, and its gradients.
 //
 //   h = x + res,  rstd = (mean h^2 + eps)^-1/2,  y = h rstd w
-//   8 bits: scale = max |y| / 448 over a row or over 128 columns, q = e4m3(y / scale)
+//   8 bits: scale = max |y| / 448 over a row or over 128 columns, q = e4m3(y (1 / scale))
 //   backward, g = w dy, xh = h rstd: dx = dh + rstd (g - xh mean(g xh)), dw = sum_rows dy xh
 //
 // A row is read once: TPR threads hold it in registers (EPT elements each, 16-byte
@@ -18,7 +18,8 @@
 namespace kdn {
 namespace {
 
-constexpr float kF8Max = 448.f;  // largest finite e4m3 value
+constexpr float kF8Max = 448.f;           // largest finite e4m3 value
+constexpr float kMinNormal = 0x1p-126f;  // of float32
 
 template <typename DT> constexpr int EV = 16 / (int)sizeof(DT);  // elements of a 16-byte vector
 
@@ -143,7 +144,16 @@ __global__ void __launch_bounds__(CTA<TPR>) k_add_rmsnorm(const NormArgs a) {
       // an all-zero block has scale 1; so has one whose magnitudes are not finite (its
       // elements are NaN: a row with an infinity or a NaN has no finite norm)
       const bool ok = big > 0.f && big < INFINITY;
-      const float scale = ok ? big / kF8Max : 1.f, inv = 1.f / scale;
+      float scale = ok ? big / kF8Max : 1.f, up = 1.f;
+      if (scale < kMinNormal) {
+        // its reciprocal may be infinite and itself zero: rounded up, so that no element
+        // passes 448, and divided by with both moved up by an (exact) power of two
+        scale = __fdiv_ru(big, kF8Max);
+        up = 0x1p100f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[i][e] *= up;
+      }
+      const float inv = 1.f / (scale * up);
       if (c < nv) {
         unsigned char q[V];
 #pragma unroll

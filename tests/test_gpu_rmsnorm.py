@@ -114,6 +114,35 @@ def test_eight_bit_special_rows(kdn):
         assert torch.equal(alone[0].float()[0], y[5]) and torch.equal(alone[3][0], s[5])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("block", [0, 128])
+@pytest.mark.parametrize("size", [1e-30, 1e-35, 1e-36, 1e-37, 2e-38, 1e-39, 1e-40, 3e-43, 3e-45])
+def test_eight_bit_tiny_blocks(kdn, dtype, block, size):
+    """Blocks whose largest magnitude is far below one, zeros among their elements: the scale
+    is positive and y is q * scale as everywhere else.  Below float32's normal range each
+    product of y = h (rstd w) is off by up to 2^-150, and the scale by 2^-149."""
+    D, rows = 384, 5
+    x, = rand(11, (rows, D), dtype=dtype)
+    x[:, 3::7] = 0
+    w = (rand(12, (D,), dtype=F32)[0] * size).to(dtype)
+    if block:
+        w[128:256], = rand(13, (128,), dtype=dtype)  # the block between them is of order one
+    y, _, _, scales = kdn.kdn_add_rmsnorm_fwd(x, w, eps=EPS, out_dtype=F8, block=block)
+    H, R, Y = define(x, w, None)
+    b = block or D
+    s32, tiny = 8 * math.sqrt(D) * 2.0 ** -24 + 2.0 ** -20, 2.0 ** -150 * (H.abs() + 1)
+    amax = Y.abs().view(rows, D // b, b).amax(-1)
+    assert torch.equal(scales == 1, amax == 0)
+    within("scales", torch.where(amax > 0, scales, 0), amax / 448,
+           s32 * amax / 448 + 2.0 ** -149 + float(tiny.max()) / 448)
+    assert (scales > 0).all()
+    wide = scales.double().repeat_interleave(b, 1)
+    z = Y / wide
+    step = torch.exp2(torch.floor(torch.log2(z.abs().clamp_min(2.0 ** -6))) - 3)
+    within("q", y.double(), z, step / 2 + s32 * z.abs() + tiny / wide)
+    assert float(y.double().abs().max()) <= 448 and not y.float()[Y == 0].any()
+
+
 def test_in_place_shapes_streams_and_bits(kdn):
     x, res, dy, dh = rand(3, *[(2, 37, 2304)] * 4)
     w, = rand(4, (2304,))
