@@ -14,6 +14,11 @@ Layouts follow the C ABI: q, k [B,T,H,dk]; v [B,T,H,dv]; r [B,T,H];
 diag g, omega [B,T,H,dk]; iso omega [B,T,H], g [B,T,H,dk] or [B,T,H];
 S0 [B,H,dk,dv] float32; p0 diag [B,H,dk], iso [B,H] float32.
 
+Streams: a call runs on the current stream, or on ``stream=``, which the caller orders
+behind whatever made the inputs.  With ``stream=`` the workspace and outputs that the call
+makes are that stream's memory and may be dropped at any time; the caller's own tensors stay
+the caller's to keep until the stream has passed the call.
+
 The hybrid layer's operators (sliding-window attention with sinks, the residual RMS
 norm) are at the end of the module, with their layouts.
 """
@@ -145,6 +150,25 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _on(fn, args):
+    """fn(**args) with args["stream"] as the current stream.  What the call makes (workspace,
+    outputs) then comes from that stream's memory, which is handed out again in the stream's own
+    order and so never while the call's kernels still use it.  The outputs are recorded on the
+    caller's stream too, so that they may be read and dropped there."""
+    stream = args.pop("stream")
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    home = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = fn(**args)
+    made = out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,)
+    for t in made:
+        if t is not None:
+            t.record_stream(home)
+    return out
+
+
 def _code(dtype):
     return _DTYPES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
 
@@ -251,8 +275,10 @@ def alloc_workspace(desc, variant, backward=False, device=None):
 
 
 def _fwd(name, variant, q, k, v, g, omega, r, S0, p0, *, chunk, mu, scale, o, ST, pT,
-         want_state, workspace, stream, out_dtype,
-         gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT):
+         want_state, workspace, out_dtype,
+         gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
+    if stream is not None:
+        return _on(_fwd, locals())
     _check_inputs(variant, q, k, v, g, omega, r)
     desc = _desc_from(variant, q, v, g, chunk=chunk, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
@@ -304,8 +330,10 @@ def kdn_iso_fwd(q, k, v, g, omega, r, S0=None, p0=None, *, chunk=0, mu=None, sca
 
 
 def _bwd(name, variant, q, k, v, g, omega, r, S0, p0, dO, dST, dpT, *, chunk, mu, scale,
-         grads, want_state_grads, workspace, stream, out_dtype,
-         gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT):
+         grads, want_state_grads, workspace, out_dtype,
+         gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
+    if stream is not None:
+        return _on(_bwd, locals())
     _check_inputs(variant, q, k, v, g, omega, r, dO)
     desc = _desc_from(variant, q, v, g, chunk=chunk, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
@@ -368,8 +396,10 @@ def saved_bytes(desc: kdn_desc_t, variant: int = 0) -> int:
 
 
 def _fwd_save(name, variant, q, k, v, g, omega, r, S0, p0, *, mu, scale, o, ST, pT, saved,
-              want_state, workspace, stream, out_dtype,
-              gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT):
+              want_state, workspace, out_dtype,
+              gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
+    if stream is not None:
+        return _on(_fwd_save, locals())
     _check_inputs(variant, q, k, v, g, omega, r)
     desc = _desc_from(variant, q, v, g, chunk=0, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
@@ -426,8 +456,10 @@ def kdn_iso_fwd_save(q, k, v, g, omega, r, S0=None, p0=None, *, mu=None, scale=N
 
 
 def _bwd_saved(name, variant, q, k, v, g, omega, r, saved, dO, dST, dpT, *, mu, scale, grads,
-               want_state_grads, workspace, stream, out_dtype,
-               gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT):
+               want_state_grads, workspace, out_dtype,
+               gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
+    if stream is not None:
+        return _on(_bwd_saved, locals())
     _check_inputs(variant, q, k, v, g, omega, r, dO)
     desc = _desc_from(variant, q, v, g, chunk=0, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
@@ -484,7 +516,9 @@ def kdn_iso_bwd_saved(q, k, v, g, omega, r, saved, dO, dST=None, dpT=None, *, mu
         gates=gates, r_min=r_min)
 
 
-def _beta_eff(name, variant, k, v, g, r, saved, *, out, stream, gates, r_min):
+def _beta_eff(name, variant, k, v, g, r, saved, *, out, stream=None, gates, r_min):
+    if stream is not None:
+        return _on(_beta_eff, locals())
     desc = _desc_from(variant, k, v, g, chunk=0, mu=None, scale=None, out_dtype=torch.float32,
                       gates=gates, r_min=r_min)
     B, T, H, _ = k.shape
@@ -515,8 +549,10 @@ def kdn_iso_beta_eff(k, v, g, r, saved, *, out=None, stream=None, gates=KDN_GATE
                      gates=gates, r_min=r_min)
 
 
-def _decode(name, variant, q, k, v, g, omega, r, S, p, *, mu, scale, o, stream, out_dtype,
-            gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT):
+def _decode(name, variant, q, k, v, g, omega, r, S, p, *, mu, scale, o, out_dtype,
+            gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
+    if stream is not None:
+        return _on(_decode, locals())
     _check_inputs(variant, q, k, v, g, omega, r, tokens=False)
     B, H, dk = q.shape
     dv = v.shape[-1]
@@ -649,6 +685,8 @@ def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=
                 workspace=None, stream=None):
     """Sliding-window attention with sinks over whole sequences.  Returns (o, lse); lse is
     None with want_lse=False (kdn_swa_bwd needs it).  Rows at and past lens[b] give o = 0."""
+    if stream is not None:
+        return _on(kdn_swa_fwd, locals())
     _check_swa(q, k, v)
     B, T, H, d = q.shape
     _arg(lens, "lens", torch.int32, B, required=False)
@@ -672,6 +710,8 @@ def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, 
                 workspace=None, stream=None):
     """Gradients of kdn_swa_fwd from its o and lse.  Returns a dict dq, dk, dv (dk and dv
     summed over the query heads that share a kv head)."""
+    if stream is not None:
+        return _on(kdn_swa_bwd, locals())
     _check_swa(q, k, v)
     B, T, H, d = q.shape
     _arg(lens, "lens", torch.int32, B, required=False)
@@ -710,6 +750,8 @@ def kdn_swa_cache_fill(k, v, kc, vc, *, window, sinks=0, lens=None, stream=None)
 def kdn_swa_decode_step(q, k, v, kc, vc, pos, *, window, sinks=0, scale=None, o=None, stream=None):
     """One token of every sequence (q [B,H,d], k, v [B,Hk,d] at position pos[b]): writes its k
     and v into the cache in place and returns its attention o [B,H,d].  pos[b] < 0: idle."""
+    if stream is not None:
+        return _on(kdn_swa_decode_step, locals())
     _check_swa(q, k, v, tokens=False)
     B, H, d = q.shape
     _arg(pos, "pos", torch.int32, B)
@@ -735,6 +777,8 @@ def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=
     """h = x + res and its RMS norm y = h rstd w over the last axis.  Returns (y, h, rstd,
     scales): h is x itself without a residual; out_dtype=torch.float8_e4m3fn gives y in 8 bits
     with float32 scales per row (block=0, [..., 1]) or per 128 columns (block=128), y ~ q * scale."""
+    if stream is not None:
+        return _on(kdn_add_rmsnorm_fwd, locals())
     _arg(x, "x")
     if x.dtype not in _DTYPES:
         raise TypeError(f"x: dtype {x.dtype}, expected torch.float32 or torch.bfloat16")
@@ -775,6 +819,8 @@ def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=
 def kdn_add_rmsnorm_bwd(h, w, rstd, dy, dh=None, *, dx=None, dw=None, workspace=None, stream=None):
     """Gradients of kdn_add_rmsnorm_fwd from its h and rstd: dy is the gradient of y, dh that
     of h from the residual stream.  Returns (dx, dw): dx for x and res alike, dw [D] float32."""
+    if stream is not None:
+        return _on(kdn_add_rmsnorm_bwd, locals())
     _arg(h, "h")
     if h.dtype not in _DTYPES:
         raise TypeError(f"h: dtype {h.dtype}, expected torch.float32 or torch.bfloat16")
