@@ -116,6 +116,8 @@ EXPORTED = tuple(_SIG)
 def lib():
     """The loaded ``libkdn.so`` (ctypes), built beforehand by ``build.build()``."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -180,17 +182,17 @@ def _torch_dtype(dtype):
     return dtype if isinstance(dtype, torch.dtype) else _TORCH[int(dtype)]
 
 
-def _arg(t, name, dtype=None, numel=None, required=True):
+def _arg(t, name, dtype=None, numel=None, required=True, dev=None):
     """A tensor handed to the C ABI as a raw pointer: it must be device memory (a
-    CUDA tensor), dense in the ABI's row-major layout (contiguous), of the dtype
-    the library reads or writes there and of the element count the descriptor
-    implies.  Anything else would make the kernels read or write the wrong
+    CUDA tensor; on device ``dev`` where the call has one), dense in the ABI's row-major
+    layout (contiguous), of the dtype the library reads or writes there and of the element
+    count the descriptor implies.  Anything else would make the kernels read or write the wrong
     memory, so it is refused here, before any launch."""
     if t is None:
         if required:
             raise ValueError(f"{name} is required")
         return
-    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()
+    if (isinstance(t, torch.Tensor) and (t.is_cuda if dev is None else t.get_device() == dev) and t.is_contiguous()
             and (dtype is None or t.dtype == dtype) and (numel is None or t.numel() == numel)):
         return
     if not isinstance(t, torch.Tensor):
@@ -198,6 +200,8 @@ def _arg(t, name, dtype=None, numel=None, required=True):
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a CUDA tensor (the kernels read device memory), "
                          f"got one on {t.device}")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the call's other tensors are on cuda:{dev}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous (the C ABI's row-major layout)")
     if dtype is not None and t.dtype != dtype:
@@ -206,10 +210,21 @@ def _arg(t, name, dtype=None, numel=None, required=True):
         raise ValueError(f"{name}: {t.numel()} elements, expected {numel}")
 
 
+def _device(t, name):
+    """The device that a call's tensors share: that of its first one, and the current one, since
+    that is where the kernels are launched."""
+    _arg(t, name)
+    dev = t.get_device()
+    if torch.cuda.is_initialized() and torch._C._cuda_getDevice() != dev:
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()} "
+                         f"(make the call under torch.cuda.device({dev}))")
+    return dev
+
+
 def _check_inputs(variant, q, k, v, g, omega, r, dO=None, tokens=True):
-    """The per-token inputs (and dO): one activation dtype, the ABI's layouts.
-    ``tokens`` = False for the decode step, whose inputs drop the T axis."""
-    _arg(q, "q")
+    """The per-token inputs (and dO): one device, which is returned, one activation dtype, the
+    ABI's layouts.  ``tokens`` = False for the decode step, whose inputs drop the T axis."""
+    dev = _device(q, "q")
     if q.dtype not in _DTYPES:
         raise TypeError(f"q: dtype {q.dtype}, expected torch.float32 or torch.bfloat16")
     if q.dim() != (4 if tokens else 3):
@@ -222,9 +237,10 @@ def _check_inputs(variant, q, k, v, g, omega, r, dO=None, tokens=True):
     per_channel = variant == 0 or g.dim() == q.dim()
     for t, name, m in ((k, "k", dk), (v, "v", dv), (g, "g", dk if per_channel else 1),
                        (omega, "omega", dk if variant == 0 else 1), (r, "r", 1)):
-        _arg(t, name, q.dtype, n * m)
+        _arg(t, name, q.dtype, n * m, dev=dev)
     if dO is not None:
-        _arg(dO, "dO", q.dtype, n * dv)
+        _arg(dO, "dO", q.dtype, n * dv, dev=dev)
+    return dev
 
 
 def _state_sizes(variant, q, v, tokens=True):
@@ -233,15 +249,15 @@ def _state_sizes(variant, q, v, tokens=True):
     return B * H * dk * dv, B * H * (dk if variant == 0 else 1)
 
 
-def _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_):
+def _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_, dev):
     """Gradient buffers: one per input, its element count, the output dtype;
     dS0, dp0 and dmu (optional) in float32."""
     od = _torch_dtype(out_dtype)
     for n, x in (("dq", q), ("dk", k), ("dv", v), ("dg", g), ("domega", omega), ("dr", r)):
-        _arg(G.get(n), n, od, x.numel())
-    _arg(G.get("dS0"), "dS0", torch.float32, ns, required=False)
-    _arg(G.get("dp0"), "dp0", torch.float32, np_, required=False)
-    _arg(G.get("dmu"), "dmu", torch.float32, q.shape[0] * q.shape[2], required=False)
+        _arg(G.get(n), n, od, x.numel(), dev=dev)
+    _arg(G.get("dS0"), "dS0", torch.float32, ns, required=False, dev=dev)
+    _arg(G.get("dp0"), "dp0", torch.float32, np_, required=False, dev=dev)
+    _arg(G.get("dmu"), "dmu", torch.float32, q.shape[0] * q.shape[2], required=False, dev=dev)
 
 
 def make_desc(B, T, H, dk, dv, dtype, *, chunk=0, mu=None, scale=None,
@@ -279,15 +295,15 @@ def _fwd(name, variant, q, k, v, g, omega, r, S0, p0, *, chunk, mu, scale, o, ST
          gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
     if stream is not None:
         return _on(_fwd, locals())
-    _check_inputs(variant, q, k, v, g, omega, r)
+    on = _check_inputs(variant, q, k, v, g, omega, r)
     desc = _desc_from(variant, q, v, g, chunk=chunk, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
     B, T, H, dk = q.shape
     dv = v.shape[-1]
     dev = q.device
     ns, np_ = _state_sizes(variant, q, v)
-    _arg(S0, "S0", torch.float32, ns, required=False)
-    _arg(p0, "p0", torch.float32, np_, required=False)
+    _arg(S0, "S0", torch.float32, ns, required=False, dev=on)
+    _arg(p0, "p0", torch.float32, np_, required=False, dev=on)
     if o is None:
         o = torch.empty(B, T, H, dv, dtype=out_dtype, device=dev)
     if want_state and ST is None:
@@ -296,10 +312,10 @@ def _fwd(name, variant, q, k, v, g, omega, r, S0, p0, *, chunk, mu, scale, o, ST
         pT = torch.empty((B, H, dk) if variant == 0 else (B, H), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = alloc_workspace(desc, variant, False, dev)
-    _arg(o, "o", _torch_dtype(out_dtype), B * T * H * dv)
-    _arg(ST, "ST", torch.float32, ns, required=False)
-    _arg(pT, "pT", torch.float32, np_, required=False)
-    _arg(workspace, "workspace", torch.uint8)
+    _arg(o, "o", _torch_dtype(out_dtype), B * T * H * dv, dev=on)
+    _arg(ST, "ST", torch.float32, ns, required=False, dev=on)
+    _arg(pT, "pT", torch.float32, np_, required=False, dev=on)
+    _arg(workspace, "workspace", torch.uint8, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                               _ptr(omega), _ptr(r), _ptr(S0), _ptr(p0), _ptr(o), _ptr(ST),
                               _ptr(pT), _ptr(workspace), workspace.numel(), _stream(stream))
@@ -334,7 +350,7 @@ def _bwd(name, variant, q, k, v, g, omega, r, S0, p0, dO, dST, dpT, *, chunk, mu
          gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
     if stream is not None:
         return _on(_bwd, locals())
-    _check_inputs(variant, q, k, v, g, omega, r, dO)
+    on = _check_inputs(variant, q, k, v, g, omega, r, dO)
     desc = _desc_from(variant, q, v, g, chunk=chunk, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
     B, T, H, dk = q.shape
@@ -342,7 +358,7 @@ def _bwd(name, variant, q, k, v, g, omega, r, S0, p0, dO, dST, dpT, *, chunk, mu
     dev = q.device
     ns, np_ = _state_sizes(variant, q, v)
     for t, n, m in ((S0, "S0", ns), (p0, "p0", np_), (dST, "dST", ns), (dpT, "dpT", np_)):
-        _arg(t, n, torch.float32, m, required=False)
+        _arg(t, n, torch.float32, m, required=False, dev=on)
     if grads is None:
         grads = {n: torch.empty(x.shape, dtype=out_dtype, device=dev) for n, x in
                  (("dq", q), ("dk", k), ("dv", v), ("dg", g), ("domega", omega), ("dr", r))}
@@ -354,8 +370,8 @@ def _bwd(name, variant, q, k, v, g, omega, r, S0, p0, dO, dST, dpT, *, chunk, mu
     if workspace is None:
         workspace = alloc_workspace(desc, variant, True, dev)
     G = grads
-    _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_)
-    _arg(workspace, "workspace", torch.uint8)
+    _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_, on)
+    _arg(workspace, "workspace", torch.uint8, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                               _ptr(omega), _ptr(r), _ptr(S0), _ptr(p0), _ptr(dO), _ptr(dST),
                               _ptr(dpT), _ptr(G["dq"]), _ptr(G["dk"]), _ptr(G["dv"]),
@@ -400,15 +416,15 @@ def _fwd_save(name, variant, q, k, v, g, omega, r, S0, p0, *, mu, scale, o, ST, 
               gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
     if stream is not None:
         return _on(_fwd_save, locals())
-    _check_inputs(variant, q, k, v, g, omega, r)
+    on = _check_inputs(variant, q, k, v, g, omega, r)
     desc = _desc_from(variant, q, v, g, chunk=0, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
     B, T, H, dk = q.shape
     dv = v.shape[-1]
     dev = q.device
     ns, np_ = _state_sizes(variant, q, v)
-    _arg(S0, "S0", torch.float32, ns, required=False)
-    _arg(p0, "p0", torch.float32, np_, required=False)
+    _arg(S0, "S0", torch.float32, ns, required=False, dev=on)
+    _arg(p0, "p0", torch.float32, np_, required=False, dev=on)
     if o is None:
         o = torch.empty(B, T, H, dv, dtype=out_dtype, device=dev)
     if want_state and ST is None:
@@ -419,11 +435,11 @@ def _fwd_save(name, variant, q, k, v, g, omega, r, S0, p0, *, mu, scale, o, ST, 
         saved = torch.empty(max(saved_bytes(desc, variant), 256), dtype=torch.uint8, device=dev)
     if workspace is None:
         workspace = alloc_workspace(desc, variant, False, dev)
-    _arg(o, "o", _torch_dtype(out_dtype), B * T * H * dv)
-    _arg(ST, "ST", torch.float32, ns, required=False)
-    _arg(pT, "pT", torch.float32, np_, required=False)
-    _arg(saved, "saved", torch.uint8)
-    _arg(workspace, "workspace", torch.uint8)
+    _arg(o, "o", _torch_dtype(out_dtype), B * T * H * dv, dev=on)
+    _arg(ST, "ST", torch.float32, ns, required=False, dev=on)
+    _arg(pT, "pT", torch.float32, np_, required=False, dev=on)
+    _arg(saved, "saved", torch.uint8, dev=on)
+    _arg(workspace, "workspace", torch.uint8, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                               _ptr(omega), _ptr(r), _ptr(S0), _ptr(p0), _ptr(o), _ptr(ST),
                               _ptr(pT), _ptr(saved), saved.numel(), _ptr(workspace),
@@ -460,16 +476,16 @@ def _bwd_saved(name, variant, q, k, v, g, omega, r, saved, dO, dST, dpT, *, mu, 
                gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
     if stream is not None:
         return _on(_bwd_saved, locals())
-    _check_inputs(variant, q, k, v, g, omega, r, dO)
+    on = _check_inputs(variant, q, k, v, g, omega, r, dO)
     desc = _desc_from(variant, q, v, g, chunk=0, mu=mu, scale=scale, out_dtype=out_dtype,
                       gates=gates, r_min=r_min)
     B, T, H, dk = q.shape
     dv = v.shape[-1]
     dev = q.device
     ns, np_ = _state_sizes(variant, q, v)
-    _arg(saved, "saved", torch.uint8)
-    _arg(dST, "dST", torch.float32, ns, required=False)
-    _arg(dpT, "dpT", torch.float32, np_, required=False)
+    _arg(saved, "saved", torch.uint8, dev=on)
+    _arg(dST, "dST", torch.float32, ns, required=False, dev=on)
+    _arg(dpT, "dpT", torch.float32, np_, required=False, dev=on)
     if grads is None:
         grads = {n: torch.empty(x.shape, dtype=out_dtype, device=dev) for n, x in
                  (("dq", q), ("dk", k), ("dv", v), ("dg", g), ("domega", omega), ("dr", r))}
@@ -481,8 +497,8 @@ def _bwd_saved(name, variant, q, k, v, g, omega, r, saved, dO, dST, dpT, *, mu, 
     if workspace is None:
         workspace = alloc_workspace(desc, variant, False, dev)
     G = grads
-    _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_)
-    _arg(workspace, "workspace", torch.uint8)
+    _check_grads(G, q, k, v, g, omega, r, out_dtype, ns, np_, on)
+    _arg(workspace, "workspace", torch.uint8, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                               _ptr(omega), _ptr(r), _ptr(saved), saved.numel(), _ptr(dO),
                               _ptr(dST), _ptr(dpT), _ptr(G["dq"]), _ptr(G["dk"]),
@@ -522,12 +538,12 @@ def _beta_eff(name, variant, k, v, g, r, saved, *, out, stream=None, gates, r_mi
     desc = _desc_from(variant, k, v, g, chunk=0, mu=None, scale=None, out_dtype=torch.float32,
                       gates=gates, r_min=r_min)
     B, T, H, _ = k.shape
-    _arg(k, "k")
-    _arg(saved, "saved", torch.uint8)
-    _arg(r, "r", k.dtype, B * T * H)
+    on = _device(k, "k")
+    _arg(saved, "saved", torch.uint8, dev=on)
+    _arg(r, "r", k.dtype, B * T * H, dev=on)
     if out is None:
         out = torch.empty(B, T, H, dtype=torch.float32, device=k.device)
-    _arg(out, "out", torch.float32, B * T * H)
+    _arg(out, "out", torch.float32, B * T * H, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(saved), ctypes.c_size_t(saved.numel()),
                               _ptr(r), _ptr(out), _stream(stream))
     _check(st, name)
@@ -553,7 +569,7 @@ def _decode(name, variant, q, k, v, g, omega, r, S, p, *, mu, scale, o, out_dtyp
             gates=KDN_GATES_POST, r_min=R_MIN_DEFAULT, stream=None):
     if stream is not None:
         return _on(_decode, locals())
-    _check_inputs(variant, q, k, v, g, omega, r, tokens=False)
+    on = _check_inputs(variant, q, k, v, g, omega, r, tokens=False)
     B, H, dk = q.shape
     dv = v.shape[-1]
     pcd = 1 if variant == 0 else int(g.dim() == 3)
@@ -561,11 +577,11 @@ def _decode(name, variant, q, k, v, g, omega, r, S, p, *, mu, scale, o, out_dtyp
                      out_dtype=out_dtype,
         gates=gates, r_min=r_min)
     ns, np_ = _state_sizes(variant, q, v, tokens=False)
-    _arg(S, "S", torch.float32, ns)
-    _arg(p, "p", torch.float32, np_)
+    _arg(S, "S", torch.float32, ns, dev=on)
+    _arg(p, "p", torch.float32, np_, dev=on)
     if o is None:
         o = torch.empty(B, H, dv, dtype=out_dtype, device=q.device)
-    _arg(o, "o", _torch_dtype(out_dtype), B * H * dv)
+    _arg(o, "o", _torch_dtype(out_dtype), B * H * dv, dev=on)
     st = getattr(lib(), name)(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                               _ptr(omega), _ptr(r), _ptr(S), _ptr(p), _ptr(o), _stream(stream))
     _check(st, name)
@@ -597,15 +613,17 @@ def kdn_diag_fwd_noalloc(q, k, v, g, omega, r, S0=None, p0=None, *, o, ST=None, 
     fixed scratch array instead of a workspace, for callers that may not
     allocate device memory.  Problems needing more than
     KDN_NOALLOC_SCRATCH_BYTES of scratch are rejected.  Returns o."""
-    _check_inputs(0, q, k, v, g, omega, r)
+    if stream is not None:
+        return _on(kdn_diag_fwd_noalloc, locals())
+    on = _check_inputs(0, q, k, v, g, omega, r)
     _arg(o, "o")
     desc = _desc_from(0, q, v, g, chunk=0, mu=mu, scale=scale, out_dtype=o.dtype, gates=gates,
                       r_min=r_min)
     B, T, H, dk = q.shape
     ns, np_ = _state_sizes(0, q, v)
-    _arg(o, "o", None, B * T * H * v.shape[-1])
+    _arg(o, "o", None, B * T * H * v.shape[-1], dev=on)
     for t, n, m in ((S0, "S0", ns), (p0, "p0", np_), (ST, "ST", ns), (pT, "pT", np_)):
-        _arg(t, n, torch.float32, m, required=False)
+        _arg(t, n, torch.float32, m, required=False, dev=on)
     st = lib().kdn_diag_fwd_noalloc(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                                     _ptr(omega), _ptr(r), _ptr(S0), _ptr(p0), _ptr(o), _ptr(ST),
                                     _ptr(pT), _stream(stream))
@@ -649,13 +667,14 @@ def make_swa_desc(B, T, H, Hk, d, dtype, *, window, sinks=0, scale=None) -> kdn_
 
 
 def _check_swa(q, k, v, tokens=True):
-    """q, k, v of one dtype: [B,T,H,d] and twice [B,T,Hk,d], without T for the decode step."""
-    _arg(q, "q")
+    """q, k, v of one dtype and device, which is returned: [B,T,H,d] and twice [B,T,Hk,d], without
+    T for the decode step."""
+    dev = _device(q, "q")
     dtype, dims = q.dtype, 4 if tokens else 3
     if dtype not in _DTYPES:
         raise TypeError(f"q: dtype {dtype}, expected torch.float32 or torch.bfloat16")
-    _arg(k, "k", dtype)
-    _arg(v, "v", dtype)
+    _arg(k, "k", dtype, dev=dev)
+    _arg(v, "v", dtype, dev=dev)
     qs, ks, vs = q.shape, k.shape, v.shape
     for shape, name in ((qs, "q"), (ks, "k"), (vs, "v")):
         if len(shape) != dims:
@@ -664,21 +683,19 @@ def _check_swa(q, k, v, tokens=True):
         raise ValueError(f"k: shape {tuple(ks)} does not go with q's {tuple(qs)}")
     if vs != ks:
         raise ValueError(f"v: shape {tuple(vs)}, expected {tuple(ks)}")
+    return dev
 
 
-def _check_cache(kc, vc, k, window, sinks):
+def _check_cache(kc, vc, k, window, sinks, dev):
     shape = (k.shape[0], k.shape[-2], int(window) + int(sinks), k.shape[-1])
     for t, name in ((kc, "kc"), (vc, "vc")):
-        _arg(t, name, k.dtype)
+        _arg(t, name, k.dtype, dev=dev)
         if t.shape != shape:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
 
 
-def _swa_workspace(workspace, nbytes, device):
-    if workspace is None:
-        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
-    _arg(workspace, "workspace", torch.uint8)
-    return workspace
+def _swa_workspace(nbytes, device):
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
 def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=None, want_lse=True,
@@ -687,19 +704,22 @@ def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=
     None with want_lse=False (kdn_swa_bwd needs it).  Rows at and past lens[b] give o = 0."""
     if stream is not None:
         return _on(kdn_swa_fwd, locals())
-    _check_swa(q, k, v)
+    on = _check_swa(q, k, v)
     B, T, H, d = q.shape
-    _arg(lens, "lens", torch.int32, B, required=False)
+    _arg(lens, "lens", torch.int32, B, required=False, dev=on)
     desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if o is None:
         o = torch.empty_like(q)
     else:
-        _arg(o, "o", q.dtype, q.numel())
+        _arg(o, "o", q.dtype, q.numel(), dev=on)
     if lse is not None:
-        _arg(lse, "lse", torch.float32, B * H * T)
+        _arg(lse, "lse", torch.float32, B * H * T, dev=on)
     elif want_lse:
         lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
-    workspace = _swa_workspace(workspace, 256, q.device)
+    if workspace is None:
+        workspace = _swa_workspace(256, q.device)
+    else:
+        _arg(workspace, "workspace", torch.uint8, dev=on)
     st = lib().kdn_swa_fwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o),
                            _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "kdn_swa_fwd")
@@ -712,21 +732,22 @@ def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, 
     summed over the query heads that share a kv head)."""
     if stream is not None:
         return _on(kdn_swa_bwd, locals())
-    _check_swa(q, k, v)
+    on = _check_swa(q, k, v)
     B, T, H, d = q.shape
-    _arg(lens, "lens", torch.int32, B, required=False)
-    _arg(o, "o", q.dtype, q.numel())
-    _arg(lse, "lse", torch.float32, B * H * T)
-    _arg(dO, "dO", q.dtype, q.numel())
+    _arg(lens, "lens", torch.int32, B, required=False, dev=on)
+    _arg(o, "o", q.dtype, q.numel(), dev=on)
+    _arg(lse, "lse", torch.float32, B * H * T, dev=on)
+    _arg(dO, "dO", q.dtype, q.numel(), dev=on)
     desc = make_swa_desc(B, T, H, k.shape[2], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if grads is None:
         grads = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
     else:
         for n, x in (("dq", q), ("dk", k), ("dv", v)):
-            _arg(grads.get(n), n, q.dtype, x.numel())
+            _arg(grads.get(n), n, q.dtype, x.numel(), dev=on)
     if workspace is None:
-        workspace = _swa_workspace(None, lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc)), q.device)
-    _arg(workspace, "workspace", torch.uint8)
+        workspace = _swa_workspace(lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc)), q.device)
+    else:
+        _arg(workspace, "workspace", torch.uint8, dev=on)
     st = lib().kdn_swa_bwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o),
                            _ptr(lse), _ptr(dO), _ptr(grads["dq"]), _ptr(grads["dk"]),
                            _ptr(grads["dv"]), _ptr(workspace), workspace.numel(), _stream(stream))
@@ -737,10 +758,12 @@ def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, 
 def kdn_swa_cache_fill(k, v, kc, vc, *, window, sinks=0, lens=None, stream=None):
     """Copies the tokens of a prompt (k, v [B,T,Hk,d]) that later tokens still see into the
     decode cache; slots that no token of it belongs to keep what they hold."""
-    _check_swa(k, k, v)
+    if stream is not None:
+        return _on(kdn_swa_cache_fill, locals())
+    on = _check_swa(k, k, v)
     B, T, Hk, d = k.shape
-    _arg(lens, "lens", torch.int32, B, required=False)
-    _check_cache(kc, vc, k, window, sinks)
+    _arg(lens, "lens", torch.int32, B, required=False, dev=on)
+    _check_cache(kc, vc, k, window, sinks, on)
     desc = make_swa_desc(B, T, Hk, Hk, d, k.dtype, window=window, sinks=sinks)
     st = lib().kdn_swa_cache_fill(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(lens), _ptr(kc),
                                   _ptr(vc), _stream(stream))
@@ -752,15 +775,15 @@ def kdn_swa_decode_step(q, k, v, kc, vc, pos, *, window, sinks=0, scale=None, o=
     and v into the cache in place and returns its attention o [B,H,d].  pos[b] < 0: idle."""
     if stream is not None:
         return _on(kdn_swa_decode_step, locals())
-    _check_swa(q, k, v, tokens=False)
+    on = _check_swa(q, k, v, tokens=False)
     B, H, d = q.shape
-    _arg(pos, "pos", torch.int32, B)
-    _check_cache(kc, vc, k, window, sinks)
+    _arg(pos, "pos", torch.int32, B, dev=on)
+    _check_cache(kc, vc, k, window, sinks, on)
     desc = make_swa_desc(B, 1, H, k.shape[1], d, q.dtype, window=window, sinks=sinks, scale=scale)
     if o is None:
         o = torch.empty_like(q)
     else:
-        _arg(o, "o", q.dtype, q.numel())
+        _arg(o, "o", q.dtype, q.numel(), dev=on)
     st = lib().kdn_swa_decode_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(kc), _ptr(vc),
                                    _ptr(pos), _ptr(o), _stream(stream))
     _check(st, "kdn_swa_decode_step")
@@ -779,7 +802,7 @@ def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=
     with float32 scales per row (block=0, [..., 1]) or per 128 columns (block=128), y ~ q * scale."""
     if stream is not None:
         return _on(kdn_add_rmsnorm_fwd, locals())
-    _arg(x, "x")
+    on = _device(x, "x")
     if x.dtype not in _DTYPES:
         raise TypeError(f"x: dtype {x.dtype}, expected torch.float32 or torch.bfloat16")
     if x.dim() < 1:
@@ -790,24 +813,24 @@ def kdn_add_rmsnorm_fwd(x, w, res=None, *, eps=1e-6, out_dtype=None, block=0, y=
         raise TypeError(f"out_dtype: {out_dtype}, expected {x.dtype} or torch.float8_e4m3fn")
     shape, n = x.shape, x.numel()
     D = shape[-1]
-    _arg(w, "w", x.dtype, D)
-    _arg(res, "res", x.dtype, n, required=False)
+    _arg(w, "w", x.dtype, D, dev=on)
+    _arg(res, "res", x.dtype, n, required=False, dev=on)
     desc = _norm_desc(x, KDN_F8E4M3 if f8 else _code(x.dtype), block, eps)
     nb = -(-D // block) if block else 1
     if y is None:
         y = torch.empty_like(x, dtype=out_dtype)
     else:
-        _arg(y, "y", out_dtype, n)
+        _arg(y, "y", out_dtype, n, dev=on)
     if h is not None:
-        _arg(h, "h", x.dtype, n)
+        _arg(h, "h", x.dtype, n, dev=on)
     elif res is not None:
         h = torch.empty_like(x)
     if rstd is not None:
-        _arg(rstd, "rstd", torch.float32, desc.rows)
+        _arg(rstd, "rstd", torch.float32, desc.rows, dev=on)
     elif want_rstd:
         rstd = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
     if scales is not None:
-        _arg(scales, "scales", torch.float32, desc.rows * nb)
+        _arg(scales, "scales", torch.float32, desc.rows * nb, dev=on)
     elif f8:
         scales = torch.empty(tuple(shape[:-1]) + (nb,), dtype=torch.float32, device=x.device)
     st = lib().kdn_add_rmsnorm_fwd(ctypes.byref(desc), _ptr(x), _ptr(res), _ptr(w), _ptr(y), _ptr(h),
@@ -821,29 +844,29 @@ def kdn_add_rmsnorm_bwd(h, w, rstd, dy, dh=None, *, dx=None, dw=None, workspace=
     of h from the residual stream.  Returns (dx, dw): dx for x and res alike, dw [D] float32."""
     if stream is not None:
         return _on(kdn_add_rmsnorm_bwd, locals())
-    _arg(h, "h")
+    on = _device(h, "h")
     if h.dtype not in _DTYPES:
         raise TypeError(f"h: dtype {h.dtype}, expected torch.float32 or torch.bfloat16")
     if h.dim() < 1:
         raise ValueError("h: a scalar, expected [..., D]")
     D = h.shape[-1]
     desc = _norm_desc(h, _code(h.dtype), 0, 0.0)
-    _arg(w, "w", h.dtype, D)
-    _arg(rstd, "rstd", torch.float32, desc.rows)
-    _arg(dy, "dy", h.dtype, h.numel())
-    _arg(dh, "dh", h.dtype, h.numel(), required=False)
+    _arg(w, "w", h.dtype, D, dev=on)
+    _arg(rstd, "rstd", torch.float32, desc.rows, dev=on)
+    _arg(dy, "dy", h.dtype, h.numel(), dev=on)
+    _arg(dh, "dh", h.dtype, h.numel(), required=False, dev=on)
     if dx is None:
         dx = torch.empty_like(h)
     else:
-        _arg(dx, "dx", h.dtype, h.numel())
+        _arg(dx, "dx", h.dtype, h.numel(), dev=on)
     if dw is None:
         dw = torch.empty(D, dtype=torch.float32, device=h.device)
     else:
-        _arg(dw, "dw", torch.float32, D)
+        _arg(dw, "dw", torch.float32, D, dev=on)
     if workspace is None:
-        workspace = _swa_workspace(None, lib().kdn_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(desc)),
-                                   h.device)
-    _arg(workspace, "workspace", torch.uint8)
+        workspace = _swa_workspace(lib().kdn_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(desc)), h.device)
+    else:
+        _arg(workspace, "workspace", torch.uint8, dev=on)
     st = lib().kdn_add_rmsnorm_bwd(ctypes.byref(desc), _ptr(h), _ptr(w), _ptr(rstd), _ptr(dy), _ptr(dh),
                                    _ptr(dx), _ptr(dw), _ptr(workspace), workspace.numel(),
                                    _stream(stream))
