@@ -373,7 +373,9 @@ typedef struct {
 
 /* Workspace bytes of kdn_swa_fwd / kdn_swa_bwd (256-byte aligned, contents
    need no initialisation; its first word is the device status that
-   kdn_get_device_status reads).  0 for a descriptor that is invalid or not served. */
+   kdn_get_device_status reads).  The backward takes two floats a query head and token and at
+   most 160 MB beside them, whatever the window and the sinks.  0 for a descriptor
+   that is invalid or not served. */
 size_t kdn_swa_fwd_workspace_bytes(const kdn_swa_desc_t *desc);
 size_t kdn_swa_bwd_workspace_bytes(const kdn_swa_desc_t *desc);
 

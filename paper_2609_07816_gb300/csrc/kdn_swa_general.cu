@@ -10,6 +10,7 @@
 // floats both operands' 16-byte reads are free of bank conflicts, and two such
 // reads feed 16 multiply-adds.  The multiply-add rate bounds these kernels.
 #include <cooperative_groups.h>
+#include <math.h>
 
 #include "kdn_swa.cuh"
 
@@ -29,19 +30,31 @@ SwaSplits swa_splits(const SwaArgs &a, int BM, int BN) {
   // Iterations of a split, where whole tiles would be less than two waves of one CTA an
   // SM: the length that ends soonest, each wave taking its longest split and a fixed part
   // (first loads, last stores; about two iterations, and two more where partial sums are
-  // written and joined).  Many more splits than SMs would be bound by those sums.  Splits
-  // of a sink tile have the length of the others, or (none split) at most twice it.
-  const long long heads = (long long)a.B * a.Hk;
+  // written and joined).  Many more splits than SMs would be bound by those sums.
+  // Otherwise only a sink tile may be split, where its list is more than twice the others':
+  // into k parts that are no shorter than those, for the least of what the splits add to
+  // every SM, 4 k iterations a tile, and the list's k-th part, by which the last tile's may
+  // outlast the rest.  Gradients at H16 d128 window 128, with splits of the others' length and
+  // so: B1 T8192 4 sinks 194 and 172 us, B1 T65536 4 sinks 1321 and 1068 us (537 and 67 MB of
+  // partial sums), B8 T8192 1024 sinks 4300 and 1887 us (4.3 GB and none).
+  // Either way a call has at most 8 partial sums an SM: 160 MB.
+  const long long heads = (long long)a.B * a.Hk, sinks = heads * p.sink_tiles, most = 8 * 152;
+  int sink_whole = iters_sink;
+  if (sinks && iters_sink > 2LL * iters) {
+    const long long k = (long long)sqrt(iters_sink * 152.0 / (4.0 * sinks)), part = k < most / sinks ? k : most / sinks;
+    if (part > 1) sink_whole = cdiv(iters_sink, part) > iters ? cdiv(iters_sink, part) : iters;
+  }
   long long whole = 0;
   double best = 0;
   for (int n = 1; n <= 8 && (n == 1 || iters / n >= 2); ++n) {
-    const int per = cdiv(iters, n), per_sink = n == 1 && iters_sink <= 2 * iters ? iters_sink : per;
+    const int per = cdiv(iters, n), per_sink = n == 1 ? sink_whole : per;
     const long long blocks = (long long)p.sink_tiles * cdiv(iters_sink, per_sink) +
                              (long long)(p.tiles - p.sink_tiles) * cdiv(iters, per);
     const int longest = p.sink_tiles && per_sink > per ? per_sink : per;
     if (n == 1) whole = heads * blocks;
+    else if (whole >= 2 * 152 || heads * blocks > most) break;
     const double cost = (double)((heads * blocks + 151) / 152) * (longest + (n == 1 ? 2 : 4));
-    if (n == 1 ? true : whole < 2 * 152 && cost < 0.95 * best) {
+    if (n == 1 || cost < 0.95 * best) {
       best = cost;
       p.per = per;
       p.per_sink = per_sink;

@@ -76,6 +76,23 @@ def test_attention_refuses_bad_pointers_and_workspaces(kdn):
             assert swa_calls(kdn, desc, ws=ws, ws_bytes=m)[name]() == kdn.KDN_ERR_WORKSPACE, name
 
 
+@pytest.mark.parametrize("T,W,ns", [(65536, 128, 4), (65536, 128, 4096), (65536, 512, 4096), (8192, 128, 1024),
+                                    (1 << 21, 1, 1 << 21), (1 << 21, 16, 4), (4096, 2048, 4), (3000, 64, 3000),
+                                    (1777, 512, 16), (512, 2048, 0)])
+def test_workspace_of_the_gradients_is_bounded(kdn, T, W, ns):
+    """Two floats a query head and token, and at most 8 partial sums of 128 keys' dk and dv
+    (64 keys' in float32) for each of 152 SMs: it does not grow with the sinks."""
+    for B, H, Hk in ((1, 1, 1), (1, 16, 16), (8, 16, 2), (8, 16, 16), (1, 64, 1), (3, 40, 5)):
+        for d, dtype, tile in ((128, BF, 128), (64, BF, 128), (32, F32, 64), (128, F32, 64)):
+            desc = kdn.make_swa_desc(B, T, H, Hk, d, dtype, window=W, sinks=ns)
+            n = kdn.lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc))
+            if B * H * T >= 1 << 31:
+                assert n == 0
+                continue
+            rows = 256 + 2 * (4 * B * H * T + 255)
+            assert 0 < n <= rows + 8 * 152 * 2 * tile * d * 4, (B, H, Hk, d, dtype)
+
+
 def test_empty_problems_need_nothing(kdn):
     for B, T, H, Hk in ((0, 8, 4, 2), (1, 0, 4, 2), (1, 8, 0, 0)):
         desc = kdn.make_swa_desc(B, T, H, Hk, 64, BF, window=4)
