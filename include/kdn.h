@@ -358,8 +358,9 @@ kdn_status_t kdn_selftest_wait_timeout(void *workspace, void *stream);
  *            softmax statistics and all sums are float32; with bfloat16 the
  *            weights (and in the backward dS) are rounded to bfloat16 as operands
  *            of the second products.
- *   Sizes    d in {32, 64, 128}; H a multiple of Hk; T >= 0, at most 2^21; B, H <=
- *            65535; B*H*T <= 2^31 - 1; window >= 1, sinks >= 0, window + sinks <= 2^30.
+ *   Sizes    d in {32, 64, 128}; H a multiple of Hk (0 heads only where both are
+ *            0); T >= 0, at most 2^21; B, H <= 65535; B*H*T <= 2^31 - 1; window
+ *            >= 1, sinks >= 0, window + sinks <= 2^30.
  *   Memory   Outputs overlap neither inputs nor one another (kernels of a call overlap).
  *   Order    Every sum has a fixed order: the same call gives the same bits.
  */

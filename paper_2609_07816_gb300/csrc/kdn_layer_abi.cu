@@ -32,7 +32,8 @@ kdn_status_t fill_swa(const kdn_swa_desc_t *d, bool tokens, SwaArgs *a) {
   if (d->d <= 0 || d->window < 1 || d->sinks < 0) return KDN_ERR_INVALID_ARG;
   if (d->dtype != KDN_F32 && d->dtype != KDN_BF16) return KDN_ERR_INVALID_ARG;
   if (!isnan(d->scale) && !(d->scale > 0.f && d->scale < INFINITY)) return KDN_ERR_INVALID_ARG;
-  if (d->H > 0 && (d->Hk == 0 || d->H % d->Hk)) return KDN_ERR_INVALID_ARG;
+  // (kv heads that no query head reads would leave their gradients and cache unwritten)
+  if ((d->H == 0) != (d->Hk == 0) || (d->H && d->H % d->Hk)) return KDN_ERR_INVALID_ARG;
   if (d->d != 32 && d->d != 64 && d->d != 128) return KDN_ERR_UNSUPPORTED;
   if (d->B > 65535 || d->H > 65535) return KDN_ERR_UNSUPPORTED;
   const int T = tokens ? d->T : 1;

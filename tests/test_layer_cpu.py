@@ -57,6 +57,15 @@ def test_attention_refuses_bad_descriptors(kdn):
     assert L.kdn_swa_decode_step(None, *[FAKE] * 8) == inv
 
 
+def test_attention_refuses_kv_heads_without_query_heads(kdn):
+    """Their dk and dv (sums over no heads) and the cache would stay as they were."""
+    desc = kdn.make_swa_desc(1, 8, 0, 2, 64, BF, window=4)
+    for name, call in swa_calls(kdn, desc).items():
+        assert call() == kdn.KDN_ERR_INVALID_ARG, name
+    assert kdn.lib().kdn_swa_fwd_workspace_bytes(ctypes.byref(desc)) == 0
+    assert kdn.lib().kdn_swa_bwd_workspace_bytes(ctypes.byref(desc)) == 0
+
+
 def test_attention_refuses_bad_pointers_and_workspaces(kdn):
     desc = kdn.make_swa_desc(1, 8, 4, 2, 64, BF, window=4)
     required = {"fwd": (0, 1, 2, 4), "bwd": (0, 1, 2, 4, 5, 6, 7, 8, 9), "fill": (0, 1, 3, 4),
