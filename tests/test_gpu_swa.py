@@ -197,6 +197,30 @@ def test_gradients_against_differences(kdn):
             assert abs(x - got) <= 2e-3 * norm * N.numel() ** 0.5 / 10
 
 
+def test_gradients_against_close_differences(kdn):
+    """Central differences of the float32 kernel's own forward, each direction to 2e-3 of its
+    gradient's norm (of which a random direction's share is about one): a term of the
+    gradient that is 1 % off shows.  At e = 2^-7 the loss, N = 19200 terms near one with a
+    relative rounding of about 2^-22, is off by 2^-22 sqrt(N) / (2 e) = 2e-3, and the third
+    derivative, some ten times the gradient's norm, adds e^2 / 6 of it, 1e-4 of the norm.
+    The norms are 33 (q, k) and 41 (v): the bound is 0.066 and more."""
+    B, T, H, Hk, d, W, ns = 1, 150, 4, 2, 32, 40, 3
+    q, k, v, dO = make(21, B, T, H, Hk, d, F32)
+    o, lse = kdn.kdn_swa_fwd(q, k, v, window=W, sinks=ns)
+    G = kdn.kdn_swa_bwd(q, k, v, o, lse, dO, window=W, sinks=ns)
+    e = 2.0 ** -7
+
+    def loss(x):
+        return float((kdn.kdn_swa_fwd(*x, window=W, sinks=ns)[0].double() * dO.double()).sum())
+
+    for seed in range(4):
+        D = rand(70 + seed, q.shape, k.shape, v.shape, dtype=F32)
+        for only, name in enumerate(("dq", "dk", "dv")):
+            at = lambda s: [x + s * e * t if n == only else x for n, (x, t) in enumerate(zip((q, k, v), D))]
+            got = float((G[name].double() * D[only].double()).sum())
+            assert abs((loss(at(1)) - loss(at(-1))) / (2 * e) - got) <= 2e-3 * float(G[name].norm()), name
+
+
 def test_caller_buffers_streams_and_graphs(kdn):
     """Outputs and workspace of the caller, another stream than the current one, and a
     captured training pass whose replay sees new inputs."""
