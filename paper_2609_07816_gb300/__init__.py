@@ -148,7 +148,7 @@ def _ptr(t):
 def _stream(stream):
     # the current stream's handle without building a Stream object (3 us of a small call)
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 
