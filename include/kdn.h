@@ -354,6 +354,9 @@ kdn_status_t kdn_selftest_wait_timeout(void *workspace, void *stream);
  *   Padding  Rows at and past len see nothing and are seen by nothing: their o
  *            and gradients are 0, their lse is -inf, and what q, k, v and dO
  *            hold there (NaN included) is never used.
+ *   Values   Live tokens (before len) are taken to be finite.  A NaN or an infinity in
+ *            one's k, v, q or dO reaches what its definition names and may also reach
+ *            queries and keys that do not see it (a weight of zero times it).
  *   Dtypes   q, k, v, dO, o, the caches and the gradients have desc->dtype.  Scores,
  *            softmax statistics and all sums are float32; with bfloat16 the
  *            weights (and in the backward dS) are rounded to bfloat16 as operands

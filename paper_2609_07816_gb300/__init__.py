@@ -19,6 +19,12 @@ behind whatever made the inputs.  With ``stream=`` the workspace and outputs tha
 makes are that stream's memory and may be dropped at any time; the caller's own tensors stay
 the caller's to keep until the stream has passed the call.
 
+Device status: the tensor-core kernels wait for one another's copies and products with a
+limit.  A wait that runs out leaves the call's outputs invalid and a code in the first word of
+the workspace, not in the return value (the call is over before the kernels are).  A caller
+who wants to know passes ``workspace=`` and reads it with kdn_get_device_status, which waits
+for the stream; the status of a workspace that the call makes itself goes with it.
+
 The hybrid layer's operators (sliding-window attention with sinks, the residual RMS
 norm) are at the end of the module, with their layouts.
 """
@@ -644,6 +650,8 @@ def kdn_selftest_wait_timeout(workspace, stream=None) -> int:
 
 
 def kdn_get_device_status(workspace, stream=None) -> int:
+    """Reads and clears the status word of the last call on ``workspace`` (KDN_OK, KDN_ERR_TIMEOUT
+    or KDN_ERR_RANGE), once the stream has passed it."""
     _arg(workspace, "workspace")
     return int(lib().kdn_get_device_status(_ptr(workspace), _stream(stream)))
 
@@ -701,7 +709,8 @@ def _swa_workspace(nbytes, device):
 def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=None, want_lse=True,
                 workspace=None, stream=None):
     """Sliding-window attention with sinks over whole sequences.  Returns (o, lse); lse is
-    None with want_lse=False (kdn_swa_bwd needs it).  Rows at and past lens[b] give o = 0."""
+    None with want_lse=False (kdn_swa_bwd needs it).  Rows at and past lens[b] give o = 0.  The
+    status of a device-side wait is in ``workspace`` only (kdn_get_device_status)."""
     if stream is not None:
         return _on(kdn_swa_fwd, locals())
     on = _check_swa(q, k, v)
@@ -729,7 +738,8 @@ def kdn_swa_fwd(q, k, v, *, window, sinks=0, lens=None, scale=None, o=None, lse=
 def kdn_swa_bwd(q, k, v, o, lse, dO, *, window, sinks=0, lens=None, scale=None, grads=None,
                 workspace=None, stream=None):
     """Gradients of kdn_swa_fwd from its o and lse.  Returns a dict dq, dk, dv (dk and dv
-    summed over the query heads that share a kv head)."""
+    summed over the query heads that share a kv head).  The status of a device-side wait is in
+    ``workspace`` only (kdn_get_device_status)."""
     if stream is not None:
         return _on(kdn_swa_bwd, locals())
     on = _check_swa(q, k, v)
