@@ -161,8 +161,8 @@ def _stream(stream):
 def _on(fn, args):
     """fn(**args) with args["stream"] as the current stream.  What the call makes (workspace,
     outputs) then comes from that stream's memory, which is handed out again in the stream's own
-    order and so never while the call's kernels still use it.  The outputs are recorded on the
-    caller's stream too, so that they may be read and dropped there."""
+    order and so never while the call's kernels still use it.  The outputs that it makes are
+    recorded on the caller's stream too, so that they may be read and dropped there."""
     stream = args.pop("stream")
     if not isinstance(stream, torch.cuda.Stream):
         handle = stream.cuda_stream
@@ -170,10 +170,11 @@ def _on(fn, args):
     home = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
         out = fn(**args)
-    made = out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,)
-    for t in made:
-        if t is not None:
-            t.record_stream(home)
+    given = {id(t) for t in args.values()}  # the caller's own buffers
+    if id(out) not in given:
+        for t in out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,):
+            if t is not None and id(t) not in given:
+                t.record_stream(home)
     return out
 
 

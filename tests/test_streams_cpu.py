@@ -94,3 +94,18 @@ def test_what_a_call_makes_belongs_to_its_stream(log):
         made.clear(), recorded.clear()
         call(None)  # on the current stream: as ever
         assert len(made) == n and {s for _, s in made} == {1} and not recorded, name
+
+
+def test_the_callers_own_buffers_are_left_alone(log):
+    made, recorded = log
+    e = lambda *s, dtype=BF: torch.empty(*s, dtype=dtype, device="cuda")
+    q, lse, ws = e(2, 9, 6, 64), e(2, 6, 9, dtype=F32), e(4096, dtype=torch.uint8)
+    G = {n: e(2, 9, 6, 64) for n in ("dq", "dk", "dv")}
+    made.clear()
+    o, l = kdn.kdn_swa_fwd(q, q, q, window=4, o=q, lse=lse, workspace=ws, stream=Stream())
+    assert o is q and l is lse
+    assert kdn.kdn_swa_bwd(q, q, q, q, lse, q, window=4, grads=G, workspace=ws, stream=Stream()) is G
+    assert not made and not recorded
+    x, w = e(5, 64), e(64)
+    y, h, rstd, _ = kdn.kdn_add_rmsnorm_fwd(x, w, stream=Stream())  # h is x
+    assert h is x and [id(t) for t, _ in recorded] == [id(y), id(rstd)]
