@@ -1054,11 +1054,15 @@ _status_words = {}
 
 def _status_word(dev):
     """256 bytes a device, kept: the workspace of calls that only have a status to leave, where nobody
-    asked for it.  (Calls of any stream may write there at once; nothing reads it.)"""
+    asked for it.  (Calls of any stream may write there at once; nothing reads it.)  Its memory may have
+    been another tensor's, which kernels queued on this stream still use, and only this stream's own calls
+    come behind them: the first call waits for them once, before any other stream may write there."""
     t = _status_words.get(dev)
     if t is None:
         t = torch.empty(256, dtype=torch.uint8, device=torch.device("cuda", dev))
         if not torch.cuda.is_current_stream_capturing():  # (a graph's memory goes with it)
+            if torch.cuda.is_initialized():
+                torch.cuda.current_stream(dev).synchronize()
             _status_words[dev] = t
     return t
 
