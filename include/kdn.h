@@ -517,7 +517,7 @@ kdn_status_t kdn_rope_bwd(const kdn_rope_desc_t *desc, const unsigned long long 
             the weights and h, in the backward also of dy, dg and du).
    Values   Inputs are taken to be finite.
    Sizes    D and F multiples of 8, at most 2^20; rows at most 2^31 - 1.
-   Memory   Outputs overlap neither inputs nor one another.
+   Memory   Outputs and the workspace overlap neither inputs nor one another: KDN_ERR_INVALID_ARG otherwise.
    Order    Every sum has a fixed order: the same call gives the same bits. */
 typedef enum { KDN_ACT_SILU = 0, KDN_ACT_GELU = 1 } kdn_act_t;
 typedef struct {

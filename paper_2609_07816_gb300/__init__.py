@@ -1071,8 +1071,8 @@ def kdn_ffn_fwd(x, wg, wu, wd, *, act=KDN_ACT_SILU, g=None, u=None, h=None, y=No
                 stream=None):
     """Gated feed-forward block: g = x wg^T, u = x wu^T, h = act(g) u, y = h wd^T over the last axis, act
     KDN_ACT_SILU or KDN_ACT_GELU (the tanh form).  Returns (y, g, u, h); with want_saved=False g and u are
-    None (kdn_ffn_bwd needs them).  The status of a device-side wait is in ``workspace`` only
-    (kdn_get_device_status)."""
+    None (kdn_ffn_bwd needs them).  Outputs share no memory with inputs or one another.  The status of a
+    device-side wait is in ``workspace`` only (kdn_get_device_status)."""
     if stream is not None:
         return _on(kdn_ffn_fwd, locals())
     on, dtype, rows, D, F = _check_ffn(x, wg, wu, wd)
@@ -1106,8 +1106,8 @@ def kdn_ffn_fwd(x, wg, wu, wd, *, act=KDN_ACT_SILU, g=None, u=None, h=None, y=No
 def kdn_ffn_bwd(x, wg, wu, wd, g, u, h, dy, *, act=KDN_ACT_SILU, dw_dtype=None, grads=None, workspace=None,
                 stream=None):
     """Gradients of kdn_ffn_fwd from its g, u and h; dy is the gradient of y.  Returns a dict dx, dwg, dwu,
-    dwd; the weights' gradients have dw_dtype (x's, or torch.float32).  The status of a device-side wait is
-    in ``workspace`` only (kdn_get_device_status)."""
+    dwd; the weights' gradients have dw_dtype (x's, or torch.float32) and, like dx, share no memory with
+    inputs or one another.  The status of a device-side wait is in ``workspace`` only (kdn_get_device_status)."""
     if stream is not None:
         return _on(kdn_ffn_bwd, locals())
     on, dtype, rows, D, F = _check_ffn(x, wg, wu, wd)

@@ -27,6 +27,25 @@ bool ptrs_ok(std::initializer_list<const void *> required, std::initializer_list
   return true;
 }
 
+// Memory of a tensor (p null or n 0: there is none).
+struct Span {
+  const void *p;
+  size_t n;
+};
+// No output shares memory with another one or with an input.
+bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  const auto meet = [](const Span &a, const Span &b) {
+    return a.p && b.p && a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n;
+  };
+  for (const Span *a = outs.begin(); a != outs.end(); ++a) {
+    for (const Span *b = outs.begin(); b != a; ++b)
+      if (meet(*a, *b)) return false;
+    for (const Span &b : ins)
+      if (meet(*a, b)) return false;
+  }
+  return true;
+}
+
 // Fills `a` from the descriptor; tokens = false for the decode step (no T axis).
 kdn_status_t fill_swa(const kdn_swa_desc_t *d, bool tokens, SwaArgs *a) {
   if (!d) return KDN_ERR_INVALID_ARG;
@@ -346,6 +365,11 @@ kdn_status_t kdn_ffn_fwd(const kdn_ffn_desc_t *desc, const void *x, const void *
   if (!ptrs_ok({x, wg, wu, wd, h, y}, {g, u}) || !g != !u) return KDN_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < ffn_layout(&a, false, nullptr))
     return KDN_ERR_WORKSPACE;
+  // (h, g and u are written while x and the weights are still read, y while h and Wd are)
+  const size_t es = a.dtype == KDN_F32 ? 4 : 2, xs = es * a.rows * a.D, hs = es * a.rows * a.F, ws = es * a.D * a.F;
+  if (!apart({{g, hs}, {u, hs}, {h, hs}, {y, xs}, {workspace, ffn_layout(&a, false, nullptr)}},
+             {{x, xs}, {wg, ws}, {wu, ws}, {wd, ws}}))
+    return KDN_ERR_INVALID_ARG;
   ffn_layout(&a, false, static_cast<char *>(workspace));
   a.x = x; a.wg = wg; a.wu = wu; a.wd = wd; a.g = g; a.u = u; a.h = h; a.y = y;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -363,6 +387,12 @@ kdn_status_t kdn_ffn_bwd(const kdn_ffn_desc_t *desc, const void *x, const void *
   if (a.rows > 0 && !ptrs_ok({x, wg, wu, wd, g, u, h, dy, dx})) return KDN_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < ffn_layout(&a, true, nullptr))
     return KDN_ERR_WORKSPACE;
+  // (dx is written before the weights' gradients read x and dy)
+  const size_t es = a.dtype == KDN_F32 ? 4 : 2, xs = es * a.rows * a.D, hs = es * a.rows * a.F, ws = es * a.D * a.F;
+  const size_t dws = (size_t)(a.dw_dtype == KDN_F32 ? 4 : 2) * a.D * a.F;
+  if (!apart({{dx, xs}, {dwg, dws}, {dwu, dws}, {dwd, dws}, {workspace, ffn_layout(&a, true, nullptr)}},
+             {{x, xs}, {wg, ws}, {wu, ws}, {wd, ws}, {g, hs}, {u, hs}, {h, hs}, {dy, xs}}))
+    return KDN_ERR_INVALID_ARG;
   ffn_layout(&a, true, static_cast<char *>(workspace));
   a.x = x; a.wg = wg; a.wu = wu; a.wd = wd; a.dy = dy;
   a.g = const_cast<void *>(g); a.u = const_cast<void *>(u); a.h = const_cast<void *>(h);
