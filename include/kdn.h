@@ -515,6 +515,10 @@ kdn_status_t kdn_rope_bwd(const kdn_rope_desc_t *desc, const unsigned long long 
             With float32 and more than 16 rows a product's operands are taken as three bfloat16s, which is
             exact to 2^-27 for magnitudes above 1e-33, and the workspace holds them (6 bytes an element of x,
             the weights and h, in the backward also of dy, dg and du).
+   Sums     The tensor cores truncate: with bfloat16 a sum loses up to 2^-23 of its accumulator for every 16 terms.
+            With float32 weights' gradients an accumulator takes 512 terms, and what it holds is added in float32, rounded
+            to nearest; with bfloat16 ones and for y and dx it takes up to 65536 (or 4096 of a longer sum, through
+            float32 in the workspace), for g, u and dh all D.
    Values   Inputs are taken to be finite.
    Sizes    D and F multiples of 8, at most 2^20; rows at most 2^31 - 1.
    Memory   Outputs and the workspace overlap neither inputs nor one another: KDN_ERR_INVALID_ARG otherwise.

@@ -11,6 +11,13 @@
 //   PLAIN  a sum over up to two pairs of operands (dx = dg Wg + du Wu), or up to three problems of one
 //          launch (the weights' gradients), or parts of a K axis that leave float32 partial sums.
 //
+// Sums.  The tensor cores truncate what they add into an accumulator, always towards 0: of positive terms 7e-7 of the sum
+// is lost after 512 along K, 4e-6 after 2048, 3e-5 after 8192, 1.6e-4 after 32768 (2^-25.4 to 2^-23.6 for every 16).  A
+// float32 output's sum leaves the accumulator every 512 along K and is added, rounded to nearest, in the epilogue's
+// registers, while the products go on in the second accumulator; so do partial sums of a bfloat16 output, every 4096.
+// A bfloat16 output that would take more than 65536 along K into one accumulator (3e-4, a sixth of half a step) goes
+// through a float32 one.
+//
 // CTAs are persistent, one an SM; the accumulator is doubled, so that a tile's epilogue runs beside
 // the next one's products.  Roles: warp 0 the loads, warp 1 the products, warps 4-11 the epilogue
 // (32 rows each, columns halved); PLAIN's results go out through shared memory by TMA.
@@ -40,6 +47,7 @@ struct Work {
   int am, bm;           // A and B are stored along their own axes
   int keep;             // B is a weight matrix that L2 has room for
   int ks;               // 16s along K that a step loads and multiplies: 4, fewer where K ends before (both own)
+  int chunk;            // steps of a sum between two additions into registers (PLAIN, float32 out)
   int act;
   bf *out[3];           // GATE: g, u (null: not written), h; DGATE: dg, du
   const bf *in[2];      // DGATE: g, u
@@ -121,6 +129,7 @@ __device__ __forceinline__ void copy_async(void *dst, const void *src, bool live
 template <int BN, int EPI, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc(const __grid_constant__ Work w) {
   constexpr int NS = STAGES<BN, EPI>, SB = STAGE<BN>;
+  constexpr bool SUMS = EPI == PLAIN && F32;  // chunks of a sum are added in registers
   extern __shared__ unsigned char smraw[];
   unsigned char *sm =
       reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
@@ -222,30 +231,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
       bool ok = true;
       for (int t = pair; ok && t < w.tiles; t += pairs) {
         const Tile T = tile_of<BN, EPI>(w, t);
-        if (!(ok = wait(acc_empty + acc, acc_turn))) break;
-        tc_fence_after();
-        const uint32_t d = tb + acc * BN;
-        uint32_t more = 0;
-        bool ready = false;
-        for (int k = T.k1 - T.k0; k > 0; --k) {
-          if (!ready && !(ok = wait(full + st, turn))) break;
-          uint64_t *const bar = empty + st;
-          const uint64_t a = da + st * (SB >> 4), b = db + st * (SB >> 4);
-          if (++st == NS) {
-            st = 0;
-            turn ^= 1;
+        for (int left = T.k1 - T.k0; left > 0;) {
+          const int some = SUMS ? min(left, w.chunk) : left;
+          left -= some;
+          if (!(ok = wait(acc_empty + acc, acc_turn))) break;
+          tc_fence_after();
+          const uint32_t d = tb + acc * BN;
+          uint32_t more = 0;
+          bool ready = false;
+          for (int k = some; k > 0; --k) {
+            if (!ready && !(ok = wait(full + st, turn))) break;
+            uint64_t *const bar = empty + st;
+            const uint64_t a = da + st * (SB >> 4), b = db + st * (SB >> 4);
+            if (++st == NS) {
+              st = 0;
+              turn ^= 1;
+            }
+            umma_pair(d, a, b, id, more);
+            if (ks > 1) umma_pair(d, a + ka, b + kb, id, 1);
+            ready = k > 1 && mbar_try_wait(full + st, turn);
+            if (ks > 2) umma_pair(d, a + 2 * ka, b + 2 * kb, id, 1);
+            if (ks > 3) umma_pair(d, a + 3 * ka, b + 3 * kb, id, 1);
+            commit_pair(bar);
+            more = 1;
           }
-          umma_pair(d, a, b, id, more);
-          if (ks > 1) umma_pair(d, a + ka, b + kb, id, 1);
-          ready = k > 1 && mbar_try_wait(full + st, turn);
-          if (ks > 2) umma_pair(d, a + 2 * ka, b + 2 * kb, id, 1);
-          if (ks > 3) umma_pair(d, a + 3 * ka, b + 3 * kb, id, 1);
-          commit_pair(bar);
-          more = 1;
+          if (!ok) break;
+          commit_pair(acc_full + acc);
+          if (acc ^= 1, acc == 0) acc_turn ^= 1;
         }
-        if (!ok) break;
-        commit_pair(acc_full + acc);
-        if (acc ^= 1, acc == 0) acc_turn ^= 1;
       }
     }
   } else if (warp >= 4) {  // ------------------------------------------------ epilogue
@@ -278,40 +291,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
     int block = 0;
     if (EPI == DGATE)
       for (int c = 0; c < 2; ++c) fetch(pair, c, c);
-    int i = 0, sent = 0;
-    for (int t = pair; t < w.tiles; t += pairs, ++i) {
+    int i = 0, sent = 0;  // accumulators read, blocks sent
+    for (int t = pair; t < w.tiles; t += pairs) {
       const Tile T = tile_of<BN, EPI>(w, t);
       const int acc = i & 1;
       const uint32_t ta = tb + acc * BN + half * HALF + lanes;
-      wait_quietly(wait, acc_full + acc, (i / 2) & 1);
+      // PLAIN: block c of COLS columns, which `write` puts into a buffer, goes out
+      auto send = [&](int c, auto write) {
+        unsigned char *b = bufs + (sent++ & 1) * OUT_BYTES;  // whose last store but one has left it
+        if (lane == 0) bulk_wait_read_but1();
+        __syncwarp();
+        write(b);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          const int m = T.m + 128 * (int)rank + 32 * q, n = T.n + half * HALF + c * COLS;
+          if (m < T.p->M && n < T.p->N) store_3d(w.maps + T.p->out, b, n, m, T.split);
+          bulk_commit();  // (a group of nothing too: they are counted)
+        }
+      };
+      if constexpr (SUMS) {
+        float x[HALF];
+#pragma unroll
+        for (int j = 0; j < HALF; ++j) x[j] = 0.f;
+#pragma unroll 1
+        for (int k = T.k0; k < T.k1; k += w.chunk, ++i) {
+          const int acc = i & 1;
+          const bool last = k + w.chunk >= T.k1;
+          wait_quietly(wait, acc_full + acc, (i / 2) & 1);
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < HALF / COLS; ++c) {
+#pragma unroll
+            for (int h = 0; h < COLS; h += 16) {
+              float y[16];
+              tmem_ld16(tb + acc * BN + half * HALF + lanes + c * COLS + h, y);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) x[c * COLS + h + j] += y[j];
+            }
+            if (last)
+              send(c, [&](unsigned char *b) {
+#pragma unroll
+                for (int j = 0; j < COLS / 4; ++j)
+                  *reinterpret_cast<float4 *>(b + chunk_off(lane, j)) =
+                      *reinterpret_cast<const float4 *>(x + c * COLS + 4 * j);
+              });
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_at(in_cta(acc_empty + acc, 0));
+        }
+        continue;
+      }
+      wait_quietly(wait, acc_full + acc, (i++ / 2) & 1);
       tc_fence_after();
       if (EPI == PLAIN) {
-        const int m = T.m + 128 * (int)rank + 32 * q, n0 = T.n + half * HALF;
-        const CUtensorMap *out = w.maps + T.p->out;
 #pragma unroll 1
         for (int c = 0; c < HALF / COLS; ++c) {
-          float x[COLS];
+          float x[64];
 #pragma unroll
-          for (int j = 0; j < COLS; j += 32) tmem_ld32(ta + c * COLS + j, x + j);
-          unsigned char *b = bufs + (sent++ & 1) * OUT_BYTES;  // whose last store but one has left it
-          if (lane == 0) bulk_wait_read_but1();
-          __syncwarp();
-          tmem_ld_wait<COLS>(x);
-          if (F32) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<float4 *>(b + chunk_off(lane, j)) = *reinterpret_cast<const float4 *>(x + 4 * j);
-          } else {
+          for (int j = 0; j < 64; j += 32) tmem_ld32(ta + c * COLS + j, x + j);
+          send(c, [&](unsigned char *b) {
+            tmem_ld_wait<64>(x);
             stage32(b, lane, 0, x);
             stage32(b, lane, 4, x + 32);
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            const int n = n0 + c * COLS;
-            if (m < T.p->M && n < T.p->N) store_3d(out, b, n, m, T.split);
-            bulk_commit();  // (a group of nothing too: they are counted)
-          }
+          });
         }
       } else if (EPI == GATE) {
 #pragma unroll 1
@@ -403,6 +447,15 @@ Cut choose(long long M, long long N, int steps, int problems, bool may_split, bo
   return best;
 }
 
+// Steps of a sum that one accumulator takes: of a float32 output, of a float32 part of a bfloat16 one, of a bfloat16 one.
+// (Every 4, 8, 16: float32 gradients of weights of 2048 x 5632, 32768 tokens, 3190, 2650, 2660 us with all of the backward
+// pass, and 3e-7, 7e-7, 1.7e-6 of a sum of positive terms lost; bfloat16 ones 2580.)
+constexpr int OUT_CHUNK = 8, PART_CHUNK = 64, LONGEST = 1024;
+// Whether a product goes through float32 parts (a single one where a bfloat16 output's sum is too long).
+bool in_parts(const Spec &S, const Cut c) {
+  return c.splits > 1 || (!S.out_f32 && cut(S.sums * (long long)cut(S.K, BK), c.splits) > LONGEST);
+}
+
 // Half of L2, of which each of two dies may hold a copy.
 bool keeps(long long weights) { return weights * 2 <= 63LL << 20; }
 
@@ -428,7 +481,8 @@ kdn_status_t plain(const Spec &S, const Cut c, float *part, unsigned *status, bo
   w.nmaps = 3 * (S.problems > S.sums ? S.problems : S.sums);
   w.status = status;
   w.first = first;
-  const bool f32 = S.out_f32 || c.splits > 1;
+  const bool parts = in_parts(S, c), f32 = S.out_f32 || parts;
+  w.chunk = S.out_f32 ? OUT_CHUNK : PART_CHUNK;
   size_t at = 0;
   for (int i = 0; i < S.problems; ++i) {
     Problem &p = w.p[i];
@@ -441,7 +495,7 @@ kdn_status_t plain(const Spec &S, const Cut c, float *part, unsigned *status, bo
     w.tiles += p.tiles;
     p.out = 3 * i;
     void *out = S.out[i];
-    if (c.splits > 1) {
+    if (parts) {
       out = part + at;
       at += (size_t)c.splits * S.M[i] * S.N[i];
     }
@@ -463,7 +517,7 @@ kdn_status_t plain(const Spec &S, const Cut c, float *part, unsigned *status, bo
   kdn_status_t st;
   if (c.BN == 256) st = f32 ? launch<256, PLAIN, true>(w, s) : launch<256, PLAIN, false>(w, s);
   else st = f32 ? launch<128, PLAIN, true>(w, s) : launch<128, PLAIN, false>(w, s);
-  if (st != KDN_OK || c.splits == 1) return st;
+  if (st != KDN_OK || !parts) return st;
   return join_parts(S, c.splits, part, s);
 }
 
@@ -472,7 +526,7 @@ Cut cut_of(const Spec &S) {
 }
 size_t part_of(const Spec &S) {
   const Cut c = cut_of(S);
-  return c.splits > 1 ? (size_t)c.splits * S.M[0] * S.N[0] * S.problems : 0;
+  return in_parts(S, c) ? (size_t)c.splits * S.M[0] * S.N[0] * S.problems : 0;
 }
 
 // h (and g and u), or dg and du: the two kernels with an epilogue of their own
