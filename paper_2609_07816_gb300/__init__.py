@@ -922,6 +922,8 @@ class RopeFreqs:
 
     def __init__(self, rot, turns, mscale):
         self.rot, self.turns, self.mscale = int(rot), turns, float(mscale)
+        if not isinstance(turns, ctypes.Array) or turns._type_ is not ctypes.c_ulonglong:
+            raise TypeError("turns: expected a ctypes array of c_ulonglong")
         self.at = ctypes.addressof(turns)
         if len(turns) != self.rot // 2:
             raise ValueError(f"turns: {len(turns)} entries, expected {self.rot // 2}")

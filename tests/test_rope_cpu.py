@@ -211,3 +211,14 @@ def test_binding_devices_and_streams(fake, monkeypatch):
         with pytest.raises(ValueError, match="cuda:"):
             m.kdn_rope_fwd(**{**dict(q=q, k=k, freqs=f, pos=pos), **kw})
         assert not log
+
+
+def test_a_table_of_other_entries_is_refused(kdn):
+    """The library reads rot/2 entries of 64 bits: behind the end of an array of 32-bit ones, and the bits
+    of floating-point numbers as turns."""
+    for kind in (ctypes.c_uint32, ctypes.c_double, ctypes.c_longlong):
+        with pytest.raises(TypeError):
+            kdn.RopeFreqs(8, (kind * 4)(), 1.0)
+    with pytest.raises(TypeError):
+        kdn.RopeFreqs(8, [1, 2, 3, 4], 1.0)
+    assert kdn.RopeFreqs(8, (ctypes.c_ulonglong * 4)(), 1.0).rot == 8
