@@ -51,7 +51,7 @@ struct Work {
   int act;
   bf *out[3];           // GATE: g, u (null: not written), h; DGATE: dg, du
   const bf *in[2];      // DGATE: g, u
-  int wide;             // their rows start on 32 bytes
+  int wide;             // GATE: the outputs' rows start on 32 bytes
   int first;            // the call's first kernel: it clears the status word
   unsigned *status;
 };
@@ -552,7 +552,7 @@ kdn_status_t gate(const FfnArgs &a, bool back, bool first, cudaStream_t s) {
   p.steps[0] = steps;
   p.b[0] = 1;
   p.b[1] = 2;
-  w.wide = a.F % 16 == 0;
+  w.wide = !back && a.F % 16 == 0;
   void *const t[3] = {back ? a.dg : a.g, back ? a.du : a.u, back ? nullptr : a.h};
   for (int i = 0; i < 3; ++i) {
     w.out[i] = static_cast<bf *>(t[i]);
@@ -562,7 +562,6 @@ kdn_status_t gate(const FfnArgs &a, bool back, bool first, cudaStream_t s) {
   if (back) {
     w.in[0] = static_cast<const bf *>(a.g);
     w.in[1] = static_cast<const bf *>(a.u);
-    if ((uintptr_t)a.g % 32 || (uintptr_t)a.u % 32) w.wide = 0;
     ok = ok && map_of(w.maps + 1, a.wd, false, a.F, a.D, 1, 64, 64, false);
   } else {
     ok = ok && map_of(w.maps + 1, a.wg, false, a.D, a.F, 1, 64, c.BN / 2, false);
