@@ -184,3 +184,11 @@ def test_reference_gradients_are_the_differences(name):
         loss = lambda e: float((ref.forward(*[t + e * dirs[i] if j == i else t for j, t in enumerate(w)], name)[0] * dy).sum())
         # truncation e^2 and rounding 1e-14 / e at e = 1e-5
         assert abs((loss(1e-5) - loss(-1e-5)) / 2e-5 - float((G[n] * dirs[i]).sum())) <= 1e-7
+
+
+@pytest.mark.parametrize("D,F", [(768, 2048), (1280, 1280)])
+def test_workspace_of_long_sums(kdn, D, F):
+    """Weights' gradients in bfloat16 whose sums are not cut: of more than 65536 rows they go through float32."""
+    for rows, dw, part in ((65536, 1, 0), (65537, 1, 12 * D * F), (300000, 1, 12 * D * F), (300000, 0, 0)):
+        n = kdn.lib().kdn_ffn_bwd_workspace_bytes(ctypes.byref(desc(kdn, rows=rows, D=D, F=F, dw_dtype=dw)))
+        assert n == 256 + 2 * -(-rows * F * 2 // 256) * 256 + part, (rows, dw)

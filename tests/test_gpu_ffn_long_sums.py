@@ -45,11 +45,12 @@ def test_float32_gradients_of_weights(kdn, rows, D, F):  # noqa: F811
     assert float(((got[:want.shape[0]].double() - want).abs() / want).max()) <= tol
 
 
-@pytest.mark.parametrize("rows", [131080, 300000])
-def test_bfloat16_gradients_of_many_rows(kdn, rows):  # noqa: F811
+# (sums in several parts and, of the last two, in one)
+@pytest.mark.parametrize("rows,D,F", [(131080, 1024, 4096), (300000, 1024, 4096), (131080, 1280, 1280), (70000, 768, 2048)])
+def test_bfloat16_gradients_of_many_rows(kdn, rows, D, F):  # noqa: F811
     """A sum that is off by no more than `lost` rounds to what lies between its ends' roundings, since rounding
-    keeps the order; one that is off by more passes a boundary somewhere among 262144 elements."""
-    *a, dy = positive(rows, 1024, 4096)
+    keeps the order; one that is off by more passes a boundary somewhere among 81920 elements or more."""
+    *a, dy = positive(rows, D, F)
     got = kdn.kdn_ffn_bwd(*a, dy)["dwd"][:64]
     want = sums(dy, a[-1], 64)
     lost = 2.0 ** -15 + 8 * math.sqrt(rows / 4096) * 2.0 ** -24
