@@ -28,13 +28,13 @@ struct FfnArgs {
 //   gelu: a = g s(z), z = 2 sqrt(2/pi) (g + 0.044715 g^3), a' = s (1 + g (1 - s) dz/dg)
 constexpr float kGelu = 1.5957691216057308f, kGelu3 = 0.044715f;
 
-// Near float32's own precision, 2^-20.5 of act(g) (ex2 2^-22 and six roundings).  An error of the exponential's argument is
-// multiplied by the argument, so -|z| log2(e) is a sum of two float32s: a product's rest is exact by a fused multiply-add,
-// a sum's by Dekker's Fast2Sum (the larger term first).  A Newton step behind the reciprocal, and neither s nor 1 - s by
-// cancellation.  Where e^-|z| is below 2^-126 it is 0.
+// Near float32's own precision, 2^-20.5 of act(g) (ex2 2^-22 and six roundings).  An error of the exponential's
+// argument is multiplied by the argument, so -|z| log2(e) is a sum of two float32s: a product's rest is exact by a
+// fused multiply-add, a sum's by Dekker's Fast2Sum (the larger term first).  A Newton step behind the reciprocal, and
+// neither s nor 1 - s by cancellation.  Where e^-|z| is below 2^-126 it is 0.
 //   silu: |z| log2(e) = L |g|;  gelu: |g| (A + B g^2), A = log2(e) kGelu, B = A kGelu3
-// (gelu with z rounded once was 2^-16.4 off at g = -8; 2048 tokens of 1024 x 4096, forward with g and u 217.6 us then and
-// 219.0 now, gradients 473 and 477.)
+// (gelu with z rounded once was 2^-16.4 off at g = -8; 2048 tokens of 1024 x 4096, forward with g and u 217.6 us then
+// and 219.0 now, gradients 473 and 477.)
 template <int ACT> __device__ __forceinline__ void ffn_act_near(float g, float *a, float *da) {
   constexpr float kL = 1.44269502f, kLRest = 1.92596299e-8f, kLn2 = 0.69314718f;
   constexpr float kA = 2.30220819f, kARest = 1.29484024e-08f, kB = 0.102943242f, kBRest = -2.01619854e-09f;

@@ -11,12 +11,12 @@
 //   PLAIN  a sum over up to two pairs of operands (dx = dg Wg + du Wu), or up to three problems of one
 //          launch (the weights' gradients), or parts of a K axis that leave float32 partial sums.
 //
-// Sums.  The tensor cores truncate what they add into an accumulator, always towards 0: of positive terms 7e-7 of the sum
-// is lost after 512 along K, 4e-6 after 2048, 3e-5 after 8192, 1.6e-4 after 32768 (2^-25.4 to 2^-23.6 for every 16).  A
-// float32 output's sum leaves the accumulator every 512 along K and is added, rounded to nearest, in the epilogue's
-// registers, while the products go on in the second accumulator; so do partial sums of a bfloat16 output, every 4096.
-// A bfloat16 output that would take more than 65536 along K into one accumulator (3e-4, a sixth of half a step) goes
-// through a float32 one.
+// Sums.  The tensor cores truncate what they add into an accumulator, always towards 0: of positive terms 7e-7 of the
+// sum is lost after 512 along K, 4e-6 after 2048, 3e-5 after 8192, 1.6e-4 after 32768 (2^-25.4 to 2^-23.6 for every
+// 16).  A float32 output's sum leaves the accumulator every 512 along K and is added, rounded to nearest, in the
+// epilogue's registers, while the products go on in the second accumulator; so do partial sums of a bfloat16 output,
+// every 4096.  A bfloat16 output that would take more than 65536 along K into one accumulator (3e-4, a sixth of half
+// a step) goes through a float32 one.
 //
 // CTAs are persistent, one an SM; the accumulator is doubled, so that a tile's epilogue runs beside
 // the next one's products.  Roles: warp 0 the loads, warp 1 the products, warps 4-11 the epilogue
@@ -47,7 +47,7 @@ struct Work {
   int am, bm;           // A and B are stored along their own axes
   int keep;             // B is a weight matrix that L2 has room for
   int ks;               // 16s along K that a step loads and multiplies: 4, fewer where K ends before (both own)
-  int chunk;            // steps of a sum between two additions into registers (PLAIN, float32 out)
+  int chunk;            // SUMS: steps of a sum between two additions into registers
   int act;
   bf *out[3];           // GATE: g, u (null: not written), h; DGATE: dg, du
   const bf *in[2];      // DGATE: g, u
@@ -96,6 +96,11 @@ __device__ __forceinline__ void stage32(unsigned char *buf, int row, int first, 
 #pragma unroll
   for (int c = 0; c < 4; ++c) sm16(buf, chunk_off(row, first + c)) = fused::pack_bf8(x + 8 * c);
 }
+__device__ __forceinline__ void stage_f32(unsigned char *buf, int row, const float *x) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    *reinterpret_cast<float4 *>(buf + chunk_off(row, c)) = *reinterpret_cast<const float4 *>(x + 4 * c);
+}
 
 // 32 consecutive columns of a thread's own row, the first `n` of them (a multiple of 8): whole 32-byte sectors
 // where rows are aligned to them.  (By TMA they would stand in the way of the operands' copies: it takes
@@ -126,10 +131,11 @@ __device__ __forceinline__ void copy_async(void *dst, const void *src, bool live
                : "memory");
 }
 
-template <int BN, int EPI, bool F32>
+// SUMS: a tile's sum is longer than a chunk.  (A form of its own: its registers leave less room to the kernel that
+// starts beside it, 256 tokens of 2048 x 5632 30.5 us with it and 30.0 without.)
+template <int BN, int EPI, bool F32, bool SUMS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc(const __grid_constant__ Work w) {
   constexpr int NS = STAGES<BN, EPI>, SB = STAGE<BN>;
-  constexpr bool SUMS = EPI == PLAIN && F32;  // chunks of a sum are added in registers
   extern __shared__ unsigned char smraw[];
   unsigned char *sm =
       reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
@@ -296,7 +302,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
       const Tile T = tile_of<BN, EPI>(w, t);
       const int acc = i & 1;
       const uint32_t ta = tb + acc * BN + half * HALF + lanes;
-      // PLAIN: block c of COLS columns, which `write` puts into a buffer, goes out
+      // PLAIN: a block of COLS columns from c on, which `write` puts into a buffer, goes out
       auto send = [&](int c, auto write) {
         unsigned char *b = bufs + (sent++ & 1) * OUT_BYTES;  // whose last store but one has left it
         if (lane == 0) bulk_wait_read_but1();
@@ -305,7 +311,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
-          const int m = T.m + 128 * (int)rank + 32 * q, n = T.n + half * HALF + c * COLS;
+          const int m = T.m + 128 * (int)rank + 32 * q, n = T.n + half * HALF + c;
           if (m < T.p->M && n < T.p->N) store_3d(w.maps + T.p->out, b, n, m, T.split);
           bulk_commit();  // (a group of nothing too: they are counted)
         }
@@ -321,21 +327,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
           wait_quietly(wait, acc_full + acc, (i / 2) & 1);
           tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < HALF / COLS; ++c) {
+          for (int c = 0; c < HALF; c += 32) {
 #pragma unroll
-            for (int h = 0; h < COLS; h += 16) {
+            for (int h = c; h < c + 32; h += 16) {
               float y[16];
-              tmem_ld16(tb + acc * BN + half * HALF + lanes + c * COLS + h, y);
+              tmem_ld16(tb + acc * BN + half * HALF + lanes + h, y);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) x[c * COLS + h + j] += y[j];
+              for (int j = 0; j < 16; ++j) x[h + j] += y[j];
             }
-            if (last)
-              send(c, [&](unsigned char *b) {
-#pragma unroll
-                for (int j = 0; j < COLS / 4; ++j)
-                  *reinterpret_cast<float4 *>(b + chunk_off(lane, j)) =
-                      *reinterpret_cast<const float4 *>(x + c * COLS + 4 * j);
-              });
+            if (last) send(c, [&](unsigned char *b) { stage_f32(b, lane, x + c); });
           }
           tc_fence_before();
           __syncwarp();
@@ -347,14 +347,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_ffn_tc
       tc_fence_after();
       if (EPI == PLAIN) {
 #pragma unroll 1
-        for (int c = 0; c < HALF / COLS; ++c) {
-          float x[64];
+        for (int c = 0; c < HALF; c += COLS) {
+          float x[COLS];
 #pragma unroll
-          for (int j = 0; j < 64; j += 32) tmem_ld32(ta + c * COLS + j, x + j);
+          for (int j = 0; j < COLS; j += 32) tmem_ld32(ta + c + j, x + j);
           send(c, [&](unsigned char *b) {
-            tmem_ld_wait<64>(x);
-            stage32(b, lane, 0, x);
-            stage32(b, lane, 4, x + 32);
+            tmem_ld_wait<COLS>(x);
+            if (F32) {
+              stage_f32(b, lane, x);
+            } else {
+#pragma unroll
+              for (int j = 0; j < COLS; j += 32) stage32(b, lane, j / 8, x + j);
+            }
           });
         }
       } else if (EPI == GATE) {
@@ -447,20 +451,20 @@ Cut choose(long long M, long long N, int steps, int problems, bool may_split, bo
   return best;
 }
 
-// Steps of a sum that one accumulator takes: of a float32 output, of a float32 part of a bfloat16 one, of a bfloat16 one.
-// (Every 4, 8, 16: float32 gradients of weights of 2048 x 5632, 32768 tokens, 3190, 2650, 2660 us with all of the backward
-// pass, and 3e-7, 7e-7, 1.7e-6 of a sum of positive terms lost; bfloat16 ones 2580.)
+// Steps of a sum that one accumulator takes: of a float32 output, of a float32 part of a bfloat16 one, of a bfloat16
+// one.  (Of the first every 4, 8 and 16: the backward pass of 32768 tokens of 2048 x 5632 3190, 2620 and 2620 us, where
+// bfloat16 gradients of weights take 2500; 3e-7, 7e-7 and 1.7e-6 of a sum of positive terms lost.)
 constexpr int OUT_CHUNK = 8, PART_CHUNK = 64, LONGEST = 1024;
+// Steps of a part, at most.
+int steps_of(const Spec &S, const Cut c) { return cut(S.sums * (long long)cut(S.K, BK), c.splits); }
 // Whether a product goes through float32 parts (a single one where a bfloat16 output's sum is too long).
-bool in_parts(const Spec &S, const Cut c) {
-  return c.splits > 1 || (!S.out_f32 && cut(S.sums * (long long)cut(S.K, BK), c.splits) > LONGEST);
-}
+bool in_parts(const Spec &S, const Cut c) { return c.splits > 1 || (!S.out_f32 && steps_of(S, c) > LONGEST); }
 
 // Half of L2, of which each of two dies may hold a copy.
 bool keeps(long long weights) { return weights * 2 <= 63LL << 20; }
 
-template <int BN, int EPI, bool F32> kdn_status_t launch(const Work &w, cudaStream_t s) {
-  auto kernel = k_ffn_tc<BN, EPI, F32>;
+template <int BN, int EPI, bool F32 = false, bool SUMS = false> kdn_status_t launch(const Work &w, cudaStream_t s) {
+  auto kernel = k_ffn_tc<BN, EPI, F32, SUMS>;
   static std::atomic<unsigned long long> done{0};
   const kdn_status_t st = once_a_device(done, [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM<BN, EPI>) == cudaSuccess;
@@ -468,6 +472,11 @@ template <int BN, int EPI, bool F32> kdn_status_t launch(const Work &w, cudaStre
   if (st != KDN_OK) return st;
   const int grid = 2 * (w.tiles < PAIRS ? w.tiles : PAIRS);
   return launch_beside(kernel, dim3(grid), THREADS, SMEM<BN, EPI>, s, w);
+}
+
+template <int BN> kdn_status_t launch_plain(const Work &w, bool f32, bool sums, cudaStream_t s) {
+  if (sums) return launch<BN, PLAIN, true, true>(w, s);
+  return f32 ? launch<BN, PLAIN, true>(w, s) : launch<BN, PLAIN>(w, s);
 }
 
 kdn_status_t plain(const Spec &S, const Cut c, float *part, unsigned *status, bool first, cudaStream_t s) {
@@ -514,9 +523,8 @@ kdn_status_t plain(const Spec &S, const Cut c, float *part, unsigned *status, bo
     }
   }
   if (S.sums == 2) w.maps[3] = w.maps[0];  // (a place that nothing else takes; descriptors are fetched ahead)
-  kdn_status_t st;
-  if (c.BN == 256) st = f32 ? launch<256, PLAIN, true>(w, s) : launch<256, PLAIN, false>(w, s);
-  else st = f32 ? launch<128, PLAIN, true>(w, s) : launch<128, PLAIN, false>(w, s);
+  const bool sums = f32 && steps_of(S, c) > w.chunk;
+  const kdn_status_t st = c.BN == 256 ? launch_plain<256>(w, f32, sums, s) : launch_plain<128>(w, f32, sums, s);
   if (st != KDN_OK || !parts) return st;
   return join_parts(S, c.splits, part, s);
 }
@@ -568,8 +576,8 @@ kdn_status_t gate(const FfnArgs &a, bool back, bool first, cudaStream_t s) {
     ok = ok && map_of(w.maps + 2, a.wu, false, a.D, a.F, 1, 64, c.BN / 2, false);
   }
   if (!ok) return KDN_ERR_CUDA;
-  if (back) return c.BN == 256 ? launch<256, DGATE, false>(w, s) : launch<128, DGATE, false>(w, s);
-  return c.BN == 256 ? launch<256, GATE, false>(w, s) : launch<128, GATE, false>(w, s);
+  if (back) return c.BN == 256 ? launch<256, DGATE>(w, s) : launch<128, DGATE>(w, s);
+  return c.BN == 256 ? launch<256, GATE>(w, s) : launch<128, GATE>(w, s);
 }
 
 }  // namespace
