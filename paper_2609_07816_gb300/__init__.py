@@ -25,8 +25,9 @@ the workspace, not in the return value (the call is over before the kernels are)
 who wants to know passes ``workspace=`` and reads it with kdn_get_device_status, which waits
 for the stream; the status of a workspace that the call makes itself goes with it.
 
-The hybrid layer's operators (sliding-window attention with sinks, the residual RMS
-norm, rotary positions, the gated feed-forward block) are at the end of the module, with their layouts.
+The hybrid layer's operators (sliding-window attention with sinks, the residual RMS norm,
+rotary positions, the gated feed-forward block) are at the end of the module, with their
+layouts.
 """
 from __future__ import annotations
 
@@ -218,9 +219,10 @@ def _torch_dtype(dtype):
 def _arg(t, name, dtype=None, numel=None, required=True, dev=None, strided=False):
     """A tensor handed to the C ABI as a raw pointer: it must be device memory (a
     CUDA tensor; on device ``dev`` where the call has one), dense in the ABI's row-major
-    layout (contiguous; ``strided``: the caller looks at the strides), of the dtype the library reads or
-    writes there and of the element count the descriptor implies.  Anything else would make the kernels read or write the wrong
-    memory, so it is refused here, before any launch."""
+    layout (contiguous; ``strided``: the caller looks at the strides), of the dtype the
+    library reads or writes there and of the element count the descriptor implies.  Anything
+    else would make the kernels read or write the wrong memory, so it is refused here, before
+    any launch."""
     if t is None:
         if required:
             raise ValueError(f"{name} is required")

@@ -4,6 +4,12 @@
 //   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wd^T
 //   dh = dy Wd, dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu,
 //   dWg = dg^T x, dWu = du^T x, dWd = dy^T h
+//
+// In bfloat16, what is rounded to 2^-9 before the end: h, dg and du, since the tensor cores take operands of the
+// weights' type; g and u, which the forward leaves for the backward in the activations' type.  So y is 2.3e-3 of its
+// norm off and dx, dWg and dWu 3.1e-3, where one rounding of an exact result is 1.7e-3.  Two bfloat16s for h, dg and du
+// would take twice the products that read them; g and u in float32 0.7 GB more each way for 32768 tokens of F = 5632,
+// and formed again in the backward 2.3 of the pass' 6.8 TFLOP.
 #pragma once
 
 #include "kdn_beside.cuh"
@@ -16,10 +22,10 @@ struct FfnArgs {
   int D, F, dtype, act, dw_dtype;
   const void *x, *wg, *wu, *wd, *dy;
   void *g, *u, *h, *y;             // forward's outputs; read by the backward
-  void *dg, *du;                   // [rows][F] in the workspace (bfloat16)
+  void *dg, *du;                   // [rows][F] in the workspace (bfloat16; float32 uses `planes`)
   void *dx, *dwg, *dwu, *dwd;
   unsigned *status;
-  void *planes;                    // float32: operands cut into bfloat16s
+  void *planes;                    // float32: operands cut into bfloat16s, dg and du among them; few rows: dg and du
   float *part;                     // partial sums of a product whose K axis is cut
 };
 

@@ -375,7 +375,9 @@ kdn_status_t run(Work &w, const FfnArgs &a, int M, int K, const Side *p, int n, 
 
 }  // namespace
 
-// (2048 x 5632: forward of 96 tokens 29 us here and 30 by tiles of 256, of 128 33 and 31; gradients of 128 57 and 62.)
+// (2048 x 5632: forward of 96 tokens 29 us here and 30 by tiles of 256, of 128 33 and 31; gradients of 128 57 and 62.
+// At other sizes the two forms differ little there, but for the forward of small weights: 520 x 1400, forward of 96 here
+// 12 and of 97 there 19, gradients of 128 here and 129 there 27; 4096 x 8192, 57 and 52, 121 and 125.)
 // A hidden axis beyond 65536 would take more than that along K into one accumulator (dx 2 F into two or more).
 bool ffn_few_rows(const FfnArgs &a, bool back) { return a.rows <= (back ? 128 : 96) && a.F <= 65536; }
 

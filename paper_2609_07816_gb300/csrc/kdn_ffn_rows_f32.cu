@@ -8,10 +8,10 @@
 //          the rows; a second kernel adds the parts in order: dh, and with g and u dg and du; dx
 //   outer  C[m, n] = sum_t A(t, m) B(t, n): the weights' gradients
 // Weights of 3272 x 8192 (322 MB): 1 token 61 us forward (5.3 TB/s) and 120 of gradients, which write as much as they
-// read (writes alone reach 4 TB/s); 16 tokens 112 and 171, where dot is bound by its instructions (two CTAs an SM
-// of four warps, a 16-byte read of a token for eight double multiply-adds).  The tensor cores' form takes 290 and
-// 396, and 17 tokens of 520 x 1400 25 and 43 us where 12 take 12 and 23 here.  Above 16 the sums do not fit a
-// thread's registers.
+// read (writes alone reach 4 TB/s); 16 tokens 112 and 171, where dot waits for shared memory and for itself (two CTAs an
+// SM of four warps, a 16-byte read of a token for eight double multiply-adds; FMA pipe 19 %).  The tensor cores' form
+// takes 290 and 396, and 17 tokens of 520 x 1400 25 and 43 us where 12 take 12 and 23 here.  Above 16 the sums do not
+// fit a thread's registers; a second pass over the weights for 17 to 32 tokens has not been tried.
 #include "kdn_ffn.cuh"
 
 namespace kdn {

@@ -1,7 +1,7 @@
 // kdn_layer_abi.cu -- the extern "C" entry points of the hybrid layer's operators
 // (declared in include/kdn.h): sliding-window attention with sinks, the residual RMS
-// norm, rotary positions and the gated feed-forward block.  Argument validation, workspace carve-up and dispatch; nothing here
-// allocates memory.
+// norm, rotary positions and the gated feed-forward block.  Argument validation, workspace
+// carve-up and dispatch; nothing here allocates memory.
 #include <math.h>
 
 #include <initializer_list>

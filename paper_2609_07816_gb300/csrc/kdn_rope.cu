@@ -10,8 +10,10 @@
 // A CTA takes TT tokens.  Its threads first issue the loads of their units (a unit is what one
 // thread turns: a 16-byte vector of either half, or one vector of neighbouring pairs), then form the
 // tokens' cosines and sines once for all heads into shared memory while the loads fly.
-// HBM traffic bounds it: 86 us a direction for 8 x 4096 tokens of 16 + 16 heads of 128 in bfloat16, 6.2 TB/s of the
-// 6.8 of a copy.
+// HBM traffic bounds it where whole heads are turned: 86 us a direction for 8 x 4096 tokens of 16 + 16 heads of 128 in
+// bfloat16, 6.2 TB/s of the 6.8 of a copy.  Instructions do where most vectors are only copied or cleared: 8 x 1777 tokens
+// of 18 + 3 heads, 32 of 128 channels turned, padded, 29 us with 75 % of the issue slots taken (a vector's place is
+// formed twice, and its token's length looked up).
 #include "kdn_beside.cuh"
 #include "kdn_fastdiv.cuh"
 #include "kdn_rope.cuh"
