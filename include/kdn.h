@@ -486,7 +486,7 @@ kdn_status_t kdn_rope_freqs(const kdn_rope_freqs_t *f, unsigned long long *turns
    Sizes    d a multiple of 8, at most 256; rot even, 2..d; T at most 2^21; H, Hk <= 65535;
             B*T <= 2^31 - 1.
    Memory   qo may be q (with the same row distance) and ko may be k; otherwise outputs overlap
-            neither inputs nor one another. */
+            neither inputs nor one another (KDN_ERR_INVALID_ARG). */
 typedef struct {
   int B, T, H, Hk, d;
   int rot;

@@ -1024,7 +1024,8 @@ def kdn_rope_fwd(q, k, freqs, *, pos=None, lens=None, interleaved=False, qo=None
     """Queries and keys (k may be None) turned by their positions: ``pos`` [B] those of the
     sequences' first tokens (None: 0), or [B,T] those of all tokens.  Of each head the first freqs.rot
     channels are turned in pairs (i, i + rot/2), or (2i, 2i + 1) when interleaved.  Returns (qo, ko),
-    0 at and past lens[b].  qo may be q and ko may be k."""
+    0 at and past lens[b].  qo may be q and ko may be k; otherwise outputs share no memory with inputs or
+    one another."""
     return _rope(False, q, k, freqs, qo, ko, pos, lens, interleaved, stream)
 
 

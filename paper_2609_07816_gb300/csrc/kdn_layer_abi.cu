@@ -141,6 +141,19 @@ kdn_status_t fill_rope(const kdn_rope_desc_t *d, const unsigned long long *turns
   return KDN_OK;
 }
 
+// Whether two tensors of `rows` rows share memory: `w` bytes a row, `ld` bytes from one to the next.
+struct Rows {
+  const void *p;
+  long long ld, w;
+};
+bool rows_meet(const Rows &a, const Rows &b, long long rows) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  if (a.w == 0 || b.w == 0 || x >= y + (rows - 1) * b.ld + b.w || y >= x + (rows - 1) * a.ld + a.w) return false;
+  if (rows == 1 || a.ld != b.ld) return true;
+  const long long d = ((long long)(y - x) % a.ld + a.ld) % a.ld;  // heads of one projection lie beside one another
+  return d < a.w || d + b.w > a.ld;
+}
+
 // One direction: `back` reads the outputs' gradients and writes the inputs'.
 kdn_status_t rope(const kdn_rope_desc_t *desc, const unsigned long long *turns, bool back, const void *q,
                   const void *k, const int *pos, const int *lens, void *qo, void *ko, void *stream) {
@@ -161,6 +174,14 @@ kdn_status_t rope(const kdn_rope_desc_t *desc, const unsigned long long *turns, 
     a.ldo[i] = out[i] ? out[i] : dense[i];
     // a row would be written where another one is still to be read
     if (dense[i] && a.in[i] == a.out[i] && a.ldi[i] != a.ldo[i]) return KDN_ERR_INVALID_ARG;
+  }
+  const long long es = a.dtype == KDN_F32 ? 4 : 2, rows = (long long)a.B * a.T;
+  for (int i = 0; i < 2; ++i) {
+    const Rows out{a.out[i], a.ldo[i] * es, dense[i] * es};
+    if (i && rows_meet(out, {a.out[0], a.ldo[0] * es, dense[0] * es}, rows)) return KDN_ERR_INVALID_ARG;
+    for (int j = 0; j < 2; ++j)
+      if (!(i == j && a.in[i] == a.out[i]) && rows_meet(out, {a.in[j], a.ldi[j] * es, dense[j] * es}, rows))
+        return KDN_ERR_INVALID_ARG;
   }
   a.pos = pos;
   a.lens = lens;
