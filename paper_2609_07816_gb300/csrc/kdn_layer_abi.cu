@@ -384,14 +384,13 @@ kdn_status_t kdn_ffn_fwd(const kdn_ffn_desc_t *desc, const void *x, const void *
   if (st != KDN_OK) return st;
   if (a.rows == 0) return KDN_OK;
   if (!ptrs_ok({x, wg, wu, wd, h, y}, {g, u}) || !g != !u) return KDN_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < ffn_layout(&a, false, nullptr))
-    return KDN_ERR_WORKSPACE;
+  const size_t need = ffn_layout(&a, false, static_cast<char *>(workspace));
+  if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < need) return KDN_ERR_WORKSPACE;
   // (h, g and u are written while x and the weights are still read, y while h and Wd are)
   const size_t es = a.dtype == KDN_F32 ? 4 : 2, xs = es * a.rows * a.D, hs = es * a.rows * a.F, ws = es * a.D * a.F;
-  if (!apart({{g, hs}, {u, hs}, {h, hs}, {y, xs}, {workspace, ffn_layout(&a, false, nullptr)}},
+  if (!apart({{g, hs}, {u, hs}, {h, hs}, {y, xs}, {workspace, need}},
              {{x, xs}, {wg, ws}, {wu, ws}, {wd, ws}}))
     return KDN_ERR_INVALID_ARG;
-  ffn_layout(&a, false, static_cast<char *>(workspace));
   a.x = x; a.wg = wg; a.wu = wu; a.wd = wd; a.g = g; a.u = u; a.h = h; a.y = y;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return a.dtype == KDN_BF16 ? launch_ffn_fwd_tc(a, s) : launch_ffn_fwd_f32(a, s);
@@ -406,15 +405,14 @@ kdn_status_t kdn_ffn_bwd(const kdn_ffn_desc_t *desc, const void *x, const void *
   // (without rows the weights' gradients are sums over nothing, and are written)
   if (!ptrs_ok({dwg, dwu, dwd})) return KDN_ERR_INVALID_ARG;
   if (a.rows > 0 && !ptrs_ok({x, wg, wu, wd, g, u, h, dy, dx})) return KDN_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < ffn_layout(&a, true, nullptr))
-    return KDN_ERR_WORKSPACE;
+  const size_t need = ffn_layout(&a, true, static_cast<char *>(workspace));
+  if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < need) return KDN_ERR_WORKSPACE;
   // (dx is written before the weights' gradients read x and dy)
   const size_t es = a.dtype == KDN_F32 ? 4 : 2, xs = es * a.rows * a.D, hs = es * a.rows * a.F, ws = es * a.D * a.F;
   const size_t dws = (size_t)(a.dw_dtype == KDN_F32 ? 4 : 2) * a.D * a.F;
-  if (!apart({{dx, xs}, {dwg, dws}, {dwu, dws}, {dwd, dws}, {workspace, ffn_layout(&a, true, nullptr)}},
+  if (!apart({{dx, xs}, {dwg, dws}, {dwu, dws}, {dwd, dws}, {workspace, need}},
              {{x, xs}, {wg, ws}, {wu, ws}, {wd, ws}, {g, hs}, {u, hs}, {h, hs}, {dy, xs}}))
     return KDN_ERR_INVALID_ARG;
-  ffn_layout(&a, true, static_cast<char *>(workspace));
   a.x = x; a.wg = wg; a.wu = wu; a.wd = wd; a.dy = dy;
   a.g = const_cast<void *>(g); a.u = const_cast<void *>(u); a.h = const_cast<void *>(h);
   a.dx = dx; a.dwg = dwg; a.dwu = dwu; a.dwd = dwd;
